@@ -30,7 +30,9 @@ APS_MAX_FORMATS = 8
 
 EXPORTS = ("aps_format_supported", "aps_layer_maxabs", "aps_layer_scales", "aps_quantize",
            "aps_sim_reduce", "aps_sim_reduce_ex", "aps_sim_reduce_codes", "aps_dequantize", "aps_lp_gemm",
-           "aps_sync_workspace_bytes", "aps_sync_route", "aps_sync", "aps_sync_noalloc", "aps_strerror")
+           "aps_sync_workspace_bytes", "aps_sync_route", "aps_sync", "aps_sync_noalloc",
+           "aps_linear_workspace_bytes", "aps_linear", "aps_linear_grad_input", "aps_linear_grad_weight",
+           "aps_activation_grad", "aps_checkpoint_save", "aps_checkpoint_load", "aps_strerror")
 
 APS_ACC_SEQUENTIAL = 0
 APS_ACC_KAHAN = 1
@@ -44,6 +46,21 @@ APS_SYNC_ROUTE_TWO_PASS = 0
 APS_SYNC_ROUTE_ONE_PASS = 1
 APS_SYNC_ROUTE_GUESS = 2
 APS_SYNC_SCRATCH_BYTES = 96 << 20
+
+APS_DTYPE_F32 = 0
+APS_DTYPE_BF16 = 1
+APS_DTYPE_F16 = 2
+APS_ACT_NONE = 0
+APS_ACT_RELU = 1
+APS_ACT_GELU = 2
+APS_ACT_SILU = 3
+APS_LINEAR_FORWARD = 0
+APS_LINEAR_GRAD_INPUT = 1
+APS_LINEAR_GRAD_WEIGHT = 2
+APS_CKPT_ROWS = 32
+APS_CKPT_COLS = 128
+APS_CKPT_MAX_EXP = 96
+APS_GRAD_ACCUMULATE = 1
 
 
 class ApsError(RuntimeError):
@@ -115,6 +132,16 @@ def lib() -> ctypes.CDLL:
             "aps_sync_route": (ctypes.c_int, [i32, i64, FP, i32, u32]),
             "aps_sync": (ctypes.c_int, [P, i32, i64, i64, P, i32, FP, i32, P, u32, P, P, P, P, ctypes.c_uint64, P]),
             "aps_sync_noalloc": (ctypes.c_int, [P, i32, i64, i64, P, i32, FP, i32, P, u32, P, P, P, P]),
+            "aps_linear_workspace_bytes": (ctypes.c_uint64, [i32, i32, i32, i32, i32]),
+            "aps_linear": (ctypes.c_int, [P, i64, P, i64, P, P, i64, P, i64, i32, i32, i32, i32, i32, aps_format,
+                                          P, i64, P, P, ctypes.c_uint64, P]),
+            "aps_linear_grad_input": (ctypes.c_int, [P, i64, P, i64, P, i64, i32, aps_format, P, i64, P, P, i64, i32,
+                                                     i32, i32, i32, P, ctypes.c_uint64, P]),
+            "aps_linear_grad_weight": (ctypes.c_int, [P, i64, aps_format, P, i64, P, P, i64, P, i32, i32, i32, i32,
+                                                      u32, P, ctypes.c_uint64, P]),
+            "aps_activation_grad": (ctypes.c_int, [P, i64, i32, aps_format, P, i64, P, P, i64, i32, i32, i32, P]),
+            "aps_checkpoint_save": (ctypes.c_int, [P, i64, i32, i32, i32, aps_format, P, i64, P, P]),
+            "aps_checkpoint_load": (ctypes.c_int, [P, i64, P, i32, i32, aps_format, i32, P, i64, i32, P]),
             "aps_strerror": (ctypes.c_char_p, [ctypes.c_int]),
         }
         for name, (res, args) in sig.items():
@@ -464,6 +491,228 @@ def code_bytes(count: int, bits: int) -> int:
     if bits <= 8:
         return count
     return 2 * count
+
+
+# ---------------------------------------------------------- linear layers
+# Activations, weights and their gradients are 2-D GPU tensors of one type
+# (float32, bfloat16 or float16) with unit column stride; a checkpoint is a
+# uint8 tensor of codes [M][C] and an int32 tensor of block words
+# [ceil(M / 32)][ceil(C / 128)].
+
+_NO_FORMAT = Format(4, 3).c()  # where a call reads no checkpoint
+
+
+@functools.lru_cache(maxsize=None)
+def _dtype_codes():
+    import torch
+    return {torch.float32: APS_DTYPE_F32, torch.bfloat16: APS_DTYPE_BF16, torch.float16: APS_DTYPE_F16}
+
+
+def _matrix(t, name: str, dtypes, dev=None, shape=None) -> int:
+    """The row stride of a 2-D GPU tensor of one of ``dtypes`` with unit column
+    stride, on ``dev`` and of ``shape``."""
+    if not getattr(t, "is_cuda", False):
+        raise ValueError(f"{name} must be a GPU tensor" + ("" if t is None else f", got {type(t).__name__}"))
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be 2-D, got {t.dim()}-D")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name} must be of dtype {' or '.join(str(d) for d in dtypes)}, got {t.dtype}")
+    if dev is not None and t.device != dev:
+        raise ValueError(f"{name} is on {t.device}, the other arrays on {dev}")
+    rows, cols = t.shape
+    if shape is not None and (rows, cols) != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
+    if rows <= 1 or cols == 0:  # an empty or one-row tensor may report any row stride
+        if cols > 1 and t.stride(1) != 1:
+            raise ValueError(f"{name} needs unit column stride")
+        return max(cols, 1)
+    if (cols > 1 and t.stride(1) != 1) or t.stride(0) < cols:
+        raise ValueError(f"{name} needs unit column stride and rows that do not overlap")
+    return t.stride(0)
+
+
+def _ckpt_words(M: int, C: int) -> tuple:
+    return (-(-M // APS_CKPT_ROWS), -(-C // APS_CKPT_COLS))
+
+
+def _ckpt(codes, ckpt_exp, dev, shape) -> int:
+    """The codes' row stride, after a check of both arrays of a checkpoint of ``shape``."""
+    ldc = _matrix(codes, "codes", _dtypes(*_U8), dev, shape)
+    _need(ckpt_exp, "ckpt_exp", _dtypes(*_I32), dev=codes.device)
+    words = _ckpt_words(*codes.shape)
+    if ckpt_exp.numel() != words[0] * words[1]:
+        raise ValueError(f"ckpt_exp has {ckpt_exp.numel()} words, a {tuple(codes.shape)} checkpoint {words[0]} x {words[1]}")
+    return ldc
+
+
+def _new_ckpt(M: int, C: int, codes, ckpt_exp, dev):
+    import torch
+    if codes is None:
+        codes = torch.empty((M, C), dtype=torch.uint8, device=dev)
+    if ckpt_exp is None:
+        ckpt_exp = torch.empty(_ckpt_words(M, C), dtype=torch.int32, device=dev)
+    return codes, ckpt_exp
+
+
+def aps_linear_workspace_bytes(op: int, M: int, N: int, K: int, dtype) -> int:
+    """Bytes of workspace of aps_linear (APS_LINEAR_FORWARD), aps_linear_grad_input
+    or aps_linear_grad_weight; ``dtype`` is a torch dtype."""
+    return int(lib().aps_linear_workspace_bytes(int(op), int(M), int(N), int(K), _dtype_codes()[dtype]))
+
+
+def _linear_workspace(op: int, M: int, N: int, K: int, dtype: int, workspace, dev):
+    """(tensor, bytes) of the call's workspace; allocated where it is missing and needed."""
+    if workspace is None:
+        import torch
+        need = int(lib().aps_linear_workspace_bytes(op, M, N, K, dtype))
+        if need == 0:
+            return None, 0
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    _need(workspace, "workspace", _dtypes(*_U8), 0, dev)
+    return workspace, workspace.numel()
+
+
+def _float_input(t, name: str) -> tuple:
+    """(row stride, the one-element tuple of its dtype, its APS_DTYPE) of an
+    activation or gradient."""
+    ld = _matrix(t, name, tuple(_dtype_codes()))
+    return ld, (t.dtype,), _dtype_codes()[t.dtype]
+
+
+def aps_linear(X, W, bias=None, residual=None, act: int = APS_ACT_NONE, Y=None, ckpt_fmt: Format | None = None,
+               codes=None, ckpt_exp=None, workspace=None, stream=None):
+    """Y = act(X W^T + bias) + residual for W [out features][in features].
+    With ``ckpt_fmt`` the pre-activation X W^T + bias is also kept in 8 bits.
+    Missing outputs are allocated here.  Returns Y, or (Y, codes, ckpt_exp)."""
+    import torch
+    ldx, T, dt = _float_input(X, "X")
+    dev = X.device
+    M, K = X.shape
+    ldw = _matrix(W, "W", T, dev)
+    N = W.shape[0]
+    if W.shape[1] != K:
+        raise ValueError(f"inner dimensions differ: X has {K} columns, W {W.shape[1]}")
+    if bias is not None:
+        _need(bias, "bias", T, N, dev)
+    ldr = 0 if residual is None else _matrix(residual, "residual", T, dev, (M, N))
+    if Y is None:
+        Y = torch.empty((M, N), dtype=X.dtype, device=dev)
+    ldy = _matrix(Y, "Y", T, dev, (M, N))
+    ldc = 0
+    if ckpt_fmt is not None:
+        codes, ckpt_exp = _new_ckpt(M, N, codes, ckpt_exp, dev)
+        ldc = _ckpt(codes, ckpt_exp, dev, (M, N))
+    elif codes is not None or ckpt_exp is not None:
+        raise ValueError("codes and ckpt_exp need ckpt_fmt")
+    ws, nbytes = _linear_workspace(APS_LINEAR_FORWARD, M, N, K, dt, workspace, dev)
+    _check("aps_linear", lib().aps_linear(
+        _ptr(X), ldx, _ptr(W), ldw, _ptr(bias), _ptr(residual), ldr, _ptr(Y), ldy, M, N, K, dt, int(act),
+        _NO_FORMAT if ckpt_fmt is None else ckpt_fmt.c(), _ptr(codes), ldc, _ptr(ckpt_exp), _ptr(ws), nbytes,
+        _stream(stream, dev)))
+    return Y if ckpt_fmt is None else (Y, codes, ckpt_exp)
+
+
+def aps_linear_grad_input(dZ, W, residual=None, act: int = APS_ACT_NONE, codes=None, ckpt_exp=None,
+                          fmt: Format | None = None, dX=None, workspace=None, stream=None):
+    """dX = (dZ W) * act'(z) + residual, z being the checkpointed
+    pre-activation that made this layer's input (none with APS_ACT_NONE)."""
+    import torch
+    ldz, T, dt = _float_input(dZ, "dZ")
+    dev = dZ.device
+    M, N = dZ.shape
+    ldw = _matrix(W, "W", T, dev)
+    K = W.shape[1]
+    if W.shape[0] != N:
+        raise ValueError(f"inner dimensions differ: dZ has {N} columns, W {W.shape[0]} rows")
+    ldr = 0 if residual is None else _matrix(residual, "residual", T, dev, (M, K))
+    if dX is None:
+        dX = torch.empty((M, K), dtype=dZ.dtype, device=dev)
+    ldx = _matrix(dX, "dX", T, dev, (M, K))
+    ldc = 0
+    if int(act) != APS_ACT_NONE:
+        if fmt is None:
+            raise ValueError("an activation's derivative needs a checkpoint: codes, ckpt_exp and fmt")
+        ldc = _ckpt(codes, ckpt_exp, dev, (M, K))
+    elif codes is not None or ckpt_exp is not None or fmt is not None:
+        raise ValueError("a checkpoint is read for an activation's derivative only: act is none")
+    ws, nbytes = _linear_workspace(APS_LINEAR_GRAD_INPUT, M, N, K, dt, workspace, dev)
+    _check("aps_linear_grad_input", lib().aps_linear_grad_input(
+        _ptr(dZ), ldz, _ptr(W), ldw, _ptr(residual), ldr, int(act), _NO_FORMAT if fmt is None else fmt.c(),
+        _ptr(codes), ldc, _ptr(ckpt_exp), _ptr(dX), ldx, M, N, K, dt, _ptr(ws), nbytes, _stream(stream, dev)))
+    return dX
+
+
+def aps_linear_grad_weight(dZ, codes, ckpt_exp, fmt: Format, dW=None, dbias=None, accumulate: bool = False,
+                           workspace=None, stream=None):
+    """dW = dZ^T X in fp32, X from its checkpoint; with a ``dbias`` tensor also
+    the column sums of dZ.  ``accumulate`` adds to dW and dbias.  dW may be a
+    view of a row of G: ``G[w, o:o + N * K].view(N, K)``."""
+    import torch
+    ldz, _, dt = _float_input(dZ, "dZ")
+    dev = dZ.device
+    M, N = dZ.shape
+    ldc = _ckpt(codes, ckpt_exp, dev, None)
+    K = codes.shape[1]
+    if codes.shape[0] != M:
+        raise ValueError(f"dZ has {M} rows, codes {codes.shape[0]}")
+    if dW is None:
+        if accumulate:
+            raise ValueError("accumulate needs dW")
+        dW = torch.empty((N, K), dtype=torch.float32, device=dev)
+    lddw = _matrix(dW, "dW", _dtypes(*_F32), dev, (N, K))
+    _need(dbias, "dbias", _dtypes(*_F32), N, dev, optional=True)
+    ws, nbytes = _linear_workspace(APS_LINEAR_GRAD_WEIGHT, M, N, K, dt, workspace, dev)
+    _check("aps_linear_grad_weight", lib().aps_linear_grad_weight(
+        _ptr(dZ), ldz, fmt.c(), _ptr(codes), ldc, _ptr(ckpt_exp), _ptr(dW), lddw, _ptr(dbias), M, N, K, dt,
+        APS_GRAD_ACCUMULATE if accumulate else 0, _ptr(ws), nbytes, _stream(stream, dev)))
+    return dW
+
+
+def aps_activation_grad(dY, codes, ckpt_exp, fmt: Format, act: int, dZ=None, stream=None):
+    """dZ = dY * act'(z), z from its checkpoint; dZ may be dY."""
+    import torch
+    ldy, T, dt = _float_input(dY, "dY")
+    dev = dY.device
+    M, C = dY.shape
+    ldc = _ckpt(codes, ckpt_exp, dev, (M, C))
+    if dZ is None:
+        dZ = torch.empty((M, C), dtype=dY.dtype, device=dev)
+    ldz = _matrix(dZ, "dZ", T, dev, (M, C))
+    _check("aps_activation_grad", lib().aps_activation_grad(
+        _ptr(dY), ldy, int(act), fmt.c(), _ptr(codes), ldc, _ptr(ckpt_exp), _ptr(dZ), ldz, M, C, dt,
+        _stream(stream, dev)))
+    return dZ
+
+
+def aps_checkpoint_save(X, fmt: Format, codes=None, ckpt_exp=None, stream=None):
+    """The 8-bit checkpoint of X: (codes, ckpt_exp)."""
+    ldx, _, dt = _float_input(X, "X")
+    dev = X.device
+    M, C = X.shape
+    codes, ckpt_exp = _new_ckpt(M, C, codes, ckpt_exp, dev)
+    ldc = _ckpt(codes, ckpt_exp, dev, (M, C))
+    _check("aps_checkpoint_save", lib().aps_checkpoint_save(_ptr(X), ldx, M, C, dt, fmt.c(), _ptr(codes), ldc,
+                                                            _ptr(ckpt_exp), _stream(stream, dev)))
+    return codes, ckpt_exp
+
+
+def aps_checkpoint_load(codes, ckpt_exp, fmt: Format, act: int = APS_ACT_NONE, X=None, dtype=None, stream=None):
+    """act(the checkpoint's values), into X or a new tensor of ``dtype``."""
+    import torch
+    ldc = _ckpt(codes, ckpt_exp, None, None)
+    dev = codes.device
+    M, C = codes.shape
+    if X is None:
+        if dtype not in _dtype_codes():
+            raise ValueError(f"dtype must be float32, bfloat16 or float16, got {dtype}")
+        X = torch.empty((M, C), dtype=dtype, device=dev)
+    elif dtype is not None and X.dtype != dtype:
+        raise ValueError(f"X is of dtype {X.dtype}, not {dtype}")
+    ldx = _matrix(X, "X", tuple(_dtype_codes()), dev, (M, C))
+    _check("aps_checkpoint_load", lib().aps_checkpoint_load(_ptr(codes), ldc, _ptr(ckpt_exp), M, C, fmt.c(), int(act),
+                                                            _ptr(X), ldx, _dtype_codes()[X.dtype],
+                                                            _stream(stream, dev)))
+    return X
 
 
 # ------------------------------------------------------------ convenience

@@ -1,0 +1,374 @@
+// aps_linear.hpp -- device code shared by the linear layer's kernels on
+// gfx950: the activations and their derivatives, the 8-bit activation
+// checkpoints, and the epilogues of the products.
+//
+// A checkpoint holds blocks of 32 rows x 128 columns.  As in Algorithm 1 (the
+// power-of-two scale from a maximum, then the cast; Sec. 3.3.3) each block's
+// exponent is ft = emax - ceil(log2 max), so that the largest magnitude
+// lands in the format's top binade without overflow; blocks instead of whole
+// layers, since one token's outliers should not cost every other token its
+// precision.  32 rows are two steps of a 16-bit matrix instruction's
+// contraction, so that the weight gradient, which contracts over the rows,
+// decodes with one scalar exponent per step.
+//
+// Every product keeps its accumulators in fp32; the result is rounded once,
+// when it is stored in its type.
+#pragma once
+
+#include "aps_common.hpp"
+
+namespace aps {
+
+enum LinOp : int32_t { OP_FWD = APS_LINEAR_FORWARD, OP_DX = APS_LINEAR_GRAD_INPUT, OP_DW = APS_LINEAR_GRAD_WEIGHT };
+
+constexpr int CK_ROWS = APS_CKPT_ROWS, CK_COLS = APS_CKPT_COLS, CK_MAX_FT = APS_CKPT_MAX_EXP;
+constexpr int CK_ODD = 1 << 16;  // a block's exponent word: the block has an INF or NaN
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// ------------------------------------------------------------------ types
+
+template <class T>
+__device__ __forceinline__ float to_f32(T v) { return (float)v; }
+
+template <class T>
+struct TypeEmax {
+    static constexpr int value = 127;
+};
+template <>
+struct TypeEmax<_Float16> {
+    static constexpr int value = 15;
+};
+
+// Four consecutive values at an address aligned for all four.
+template <class T>
+__device__ __forceinline__ void load4(const T* p, float v[4]) {
+    typedef T t4 __attribute__((ext_vector_type(4)));
+    const t4 t = *(const t4*)p;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = (float)t[i];
+}
+template <class T>
+__device__ __forceinline__ void store4(T* p, const float v[4]) {
+    typedef T t4 __attribute__((ext_vector_type(4)));
+    t4 t;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t[i] = (T)v[i];
+    *(t4*)p = t;
+}
+
+// Up to four values of a row at p, those below `have`; `vec`: the row is
+// aligned for four at once.
+template <class T>
+__device__ __forceinline__ void load_some(const T* p, int64_t have, bool vec, float v[4]) {
+    if (vec && have >= 4) {
+        load4(p, v);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = i < have ? (float)p[i] : 0.0f;
+}
+template <class T>
+__device__ __forceinline__ void store_some(T* p, int64_t have, bool vec, const float v[4]) {
+    if (vec && have >= 4) {
+        store4(p, v);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (i < have) p[i] = (T)v[i];
+}
+__device__ __forceinline__ uint32_t load_codes4(const uint8_t* p, int64_t have, bool vec) {
+    if (vec && have >= 4) return *(const uint32_t*)p;
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (i < have) w |= (uint32_t)p[i] << (8 * i);
+    return w;
+}
+__device__ __forceinline__ void store_some_codes(uint8_t* p, int64_t have, bool vec, uint32_t w) {
+    if (vec && have >= 4) {
+        *(uint32_t*)p = w;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (i < have) p[i] = (uint8_t)(w >> (8 * i));
+}
+
+// ------------------------------------------------------------ activations
+//
+// The limits at +-INF are the functions' own: arguments beyond the bound,
+// where the result is exact in fp32 already, are taken at the bound, so that
+// no INF meets a zero.  NaN fails the compares and stays.
+
+__device__ __forceinline__ float act_value(float z, int act) {
+    if (act == APS_ACT_RELU) return z < 0.0f ? 0.0f : z;
+    if (act == APS_ACT_GELU) {
+        const float c = z < -15.0f ? -15.0f : z;
+        return c * (0.5f * (1.0f + erff(c * 0.70710678118654752f)));
+    }
+    if (act == APS_ACT_SILU) {
+        const float c = z < -104.0f ? -104.0f : z;
+        return c * __builtin_amdgcn_rcpf(1.0f + expf(-c));
+    }
+    return z;
+}
+
+__device__ __forceinline__ float act_slope(float z, int act) {
+    if (act == APS_ACT_RELU) return z > 0.0f ? 1.0f : (z != z ? z : 0.0f);
+    if (act == APS_ACT_GELU) {
+        const float c = z < -15.0f ? -15.0f : (z > 15.0f ? 15.0f : z);
+        return 0.5f * (1.0f + erff(c * 0.70710678118654752f)) + c * expf(-0.5f * c * c) * 0.39894228040143268f;
+    }
+    if (act == APS_ACT_SILU) {
+        const float c = z < -104.0f ? -104.0f : (z > 104.0f ? 104.0f : z);
+        const float s = __builtin_amdgcn_rcpf(1.0f + expf(-c));
+        return s * (1.0f + c * (1.0f - s));
+    }
+    return 1.0f;
+}
+
+// ------------------------------------------------------------ checkpoints
+
+// The largest format value, times a power of two, that T holds; the format's emax.
+template <class T, bool E5>
+constexpr float ck_limit() {
+    return (E5 ? 1.75f : 1.875f) * (TypeEmax<T>::value == 15 ? 0x1p15f : 0x1p127f);
+}
+template <bool E5>
+constexpr int ck_emax() {
+    return E5 ? 15 : 7;
+}
+
+// A finite magnitude at most lim, the largest format value that T holds;
+// INF and NaN stay.
+__device__ __forceinline__ float ck_clamp(float x, float lim) {
+    return __builtin_fabsf(x) < __builtin_inff() ? __builtin_amdgcn_fmed3f(x, -lim, lim) : x;
+}
+
+// A block's maximum as an unsigned word: the largest finite magnitude's bits,
+// and in bit 31 whether an element is INF or NaN.
+__device__ __forceinline__ uint32_t ck_max_bits(float x) {
+    const uint32_t a = f2u(x) & 0x7FFFFFFFu;
+    return a < 0x7F800000u ? a : 0x80000000u;
+}
+__device__ __forceinline__ uint32_t ck_max_join(uint32_t a, uint32_t b) {
+    return max(a & 0x7FFFFFFFu, b & 0x7FFFFFFFu) | ((a | b) & 0x80000000u);
+}
+
+// The block's exponent word from its maximum.
+__device__ __forceinline__ int32_t ck_word(uint32_t mx, int emax) {
+    const uint32_t a = mx & 0x7FFFFFFFu;
+    const int ft = a ? min(emax - ceil_log2_bits(a), CK_MAX_FT) : 0;
+    return (ft & 0xFFFF) | ((mx >> 31) ? CK_ODD : 0);
+}
+__device__ __forceinline__ int ck_ft(int32_t word) { return (int)(int16_t)word; }
+
+// 2^e; the exponents of a block are within +-126 of zero
+__device__ __forceinline__ float pow2_of(int e) { return u2f((uint32_t)(e + 127) << 23); }
+
+// The codes of four scaled values.
+template <bool E5>
+__device__ __forceinline__ uint32_t ck_encode4(const float v[4]) {
+    if constexpr (E5) return encode4_e5m2(v[0], v[1], v[2], v[3]);
+    return encode4_e4m3(v[0], v[1], v[2], v[3]);
+}
+
+// 1-4-3's INF and NaN among four codes: v where a code is one.
+__device__ __forceinline__ void ck_odd_e4m3(uint32_t w, float v[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t c = (w >> (8 * i)) & 0x7Fu;
+        if (c >= 0x78u) v[i] = c > 0x78u ? __builtin_nanf("") : __builtin_copysignf(__builtin_inff(), v[i]);
+    }
+}
+
+// The values of four codes of a block.  inv = 2^-ft.
+template <bool E5>
+__device__ __forceinline__ void ck_decode4(uint32_t w, float inv, bool odd, float v[4]) {
+    f32x2 lo, hi;
+    if constexpr (E5) {
+        lo = __builtin_amdgcn_cvt_pk_f32_bf8(w, false);
+        hi = __builtin_amdgcn_cvt_pk_f32_bf8(w, true);
+    } else {
+        lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false);
+        hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+    }
+    v[0] = lo[0] * inv;
+    v[1] = lo[1] * inv;
+    v[2] = hi[0] * inv;
+    v[3] = hi[1] * inv;
+    if (!E5 && odd) ck_odd_e4m3(w, v);
+}
+
+// ------------------------------------------------------------- a product
+//
+// Every product is out[q][p] = sum over c of P[p][c] * Q[q][c], p the output's
+// contiguous axis: P is the weights or the checkpoint's codes, Q the
+// activations or the output gradients.  P and Q say where the contraction
+// runs in memory: along a row (contiguous), or from row to row.
+//
+//   forward      out Y  [M][N]: p = n, q = m, c = k: P = W along rows, Q = X along rows
+//   grad_input   out dX [M][K]: p = k, q = m, c = n: P = W row to row, Q = dZ along rows
+//   grad_weight  out dW [N][K]: p = k, q = n, c = m: P = codes row to row, Q = dZ row to row
+
+// which rows are aligned for four elements at once
+enum LinVec : uint32_t { LV_OUT = 1, LV_R = 2, LV_CODES = 4, LV_BIAS = 8, LV_ZC = 16 };
+
+struct LinArgs {
+    const void* __restrict__ P;  // weights, or codes
+    const void* __restrict__ Q;
+    int64_t ldp, ldq;            // row strides in elements
+    int64_t np, nq, nc;          // p, q and contraction lengths
+    const void* bias;            // forward, or NULL
+    const void* R;               // added residual, or NULL; may be out
+    int64_t ldr;
+    void* out;
+    int64_t ldo;
+    uint8_t* codes;              // forward: the checkpoint of z, or NULL
+    int64_t ldcodes;
+    int32_t* exps;               // its blocks' exponent words
+    const uint8_t* zc;           // grad_input: the checkpoint of z, or NULL
+    int64_t ldzc;
+    const int32_t* zexps;        // ... its exponent words (grad_weight: those of P)
+    float* dbias;                // grad_weight, or NULL
+    float* part;                 // split products: partial sums [split][nq][ldpart]
+    float* part_bias;            // ... of dbias [split][nq]
+    int64_t ldpart;
+    int32_t act;
+    int32_t split;               // pieces of the contraction
+    int64_t piece;               // contraction length of one
+    uint32_t vec;                // LinVec
+    uint32_t accumulate;         // grad_weight: add to out
+};
+
+// A wave's join of its lanes' block maxima, in every lane.
+__device__ __forceinline__ uint32_t ck_wave_max(uint32_t m) {
+#pragma unroll
+    for (int o = 32; o; o >>= 1) m = ck_max_join(m, (uint32_t)__shfl_xor((int)m, o));
+    return m;
+}
+
+// The stored result of four consecutive p of row q (the first `have` of them),
+// v being the finished sums: bias already added in the forward pass.
+template <class T, int OP, bool E5>
+__device__ __forceinline__ void lin_finish4(const LinArgs& a, int64_t q, int64_t p, int64_t have, const float v[4]) {
+    float y[4];
+    if constexpr (OP == OP_DW) {
+        float* o = (float*)a.out + q * a.ldo + p;
+        if (a.accumulate) {
+            load_some(o, have, a.vec & LV_OUT, y);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] += v[i];
+            store_some(o, have, a.vec & LV_OUT, y);
+        } else {
+            store_some(o, have, a.vec & LV_OUT, v);
+        }
+        return;
+    }
+    if constexpr (OP == OP_FWD) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = act_value(v[i], a.act);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = v[i];
+        if (a.zc) {
+            const int32_t word = a.zexps[(q / CK_ROWS) * ((a.np + CK_COLS - 1) / CK_COLS) + p / CK_COLS];
+            float z[4];
+            ck_decode4<E5>(load_codes4(a.zc + q * a.ldzc + p, have, a.vec & LV_ZC), pow2_of(-ck_ft(word)), word & CK_ODD, z);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] *= act_slope(z[i], a.act);
+        }
+    }
+    if (a.R) {
+        float r[4];
+        load_some((const T*)a.R + q * a.ldr + p, have, a.vec & LV_R, r);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] += r[i];
+    }
+    store_some((T*)a.out + q * a.ldo + p, have, a.vec & LV_OUT, y);
+}
+
+template <class T>
+__device__ __forceinline__ void lin_bias4(const LinArgs& a, int64_t p, int64_t have, float b[4]) {
+    if (a.bias)
+        load_some((const T*)a.bias + p, have, a.vec & LV_BIAS, b);
+    else
+        b[0] = b[1] = b[2] = b[3] = 0.0f;
+}
+
+// The codes of four values of z at row q, with the block's exponent known.
+template <class T, bool E5>
+__device__ __forceinline__ void lin_save4(const LinArgs& a, int64_t q, int64_t p, int64_t have, int ft, const float z[4]) {
+    constexpr float lim = ck_limit<T, E5>();
+    const float s = pow2_of(ft);
+    float v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = ck_clamp(z[i], lim) * s;
+    store_some_codes(a.codes + q * a.ldcodes + p, have, a.vec & LV_CODES, ck_encode4<E5>(v));
+}
+
+// ------------------------------------------------------------ host checks
+
+constexpr int64_t LIN_MAX_LD = (1LL << 31) - 1;
+constexpr int64_t LIN_MAX_BLOCKS = 1 << 23;  // blocks of 32 x 128: a launch's size stays within HIP's
+
+static inline int lin_elem_bytes(int dtype) { return dtype == APS_DTYPE_F32 ? 4 : 2; }
+
+static inline bool lin_aligned(const void* p, int64_t bytes) { return ((uintptr_t)p & (uintptr_t)(bytes - 1)) == 0; }
+
+static inline bool lin_act_known(int act) { return act >= APS_ACT_NONE && act <= APS_ACT_SILU; }
+
+static inline bool lin_too_large(int64_t cols, int64_t rows) {
+    return ((cols + CK_COLS - 1) / CK_COLS) * ((rows + CK_ROWS - 1) / CK_ROWS) > LIN_MAX_BLOCKS;
+}
+
+// Of a product (M, N, K), or of a matrix (M, N, 0).
+static inline int lin_check_dims(int32_t M, int32_t N, int32_t K, int32_t dtype) {
+    if (M < 0 || N < 0 || K < 0 || M > APS_MAX_GEMM_DIM || N > APS_MAX_GEMM_DIM || K > APS_MAX_GEMM_DIM)
+        return APS_ERR_SIZE;
+    if (lin_too_large(N, M) || lin_too_large(K, M) || lin_too_large(K, N)) return APS_ERR_SIZE;
+    if (dtype != APS_DTYPE_F32 && dtype != APS_DTYPE_BF16 && dtype != APS_DTYPE_F16) return APS_ERR_UNSUPPORTED;
+    return APS_OK;
+}
+
+// A matrix of rows x cols elements of `bytes`; nothing is asked of an empty one.
+static inline int lin_check_matrix(const void* p, int64_t ld, int64_t rows, int64_t cols, int bytes) {
+    if (rows == 0 || cols == 0) return APS_OK;
+    if (!p) return APS_ERR_NULL;
+    if (ld < cols || ld > LIN_MAX_LD) return APS_ERR_SIZE;
+    return lin_aligned(p, bytes) ? APS_OK : APS_ERR_ALIGN;
+}
+
+static inline int lin_check_checkpoint(aps_format f, const void* codes, int64_t ldc, const void* exps, int64_t rows,
+                                       int64_t cols, bool& e5) {
+    int st = fmt_status(f);
+    if (st != APS_OK) return st;
+    const int hw = make_fmtk(f).hw;
+    if (hw != HW_E5M2 && hw != HW_E4M3) return APS_ERR_UNSUPPORTED;
+    e5 = hw == HW_E5M2;
+    st = lin_check_matrix(codes, ldc, rows, cols, 1);
+    if (st != APS_OK) return st;
+    if (rows == 0 || cols == 0) return APS_OK;
+    if (!exps) return APS_ERR_NULL;
+    return lin_aligned(exps, 4) ? APS_OK : APS_ERR_ALIGN;
+}
+
+#define APS_LIN_TRY(x)                   \
+    do {                                 \
+        const int st_ = (x);             \
+        if (st_ != APS_OK) return st_;   \
+    } while (0)
+
+// ------------------------------------------------------------ the launches
+
+// dtype is one of APS_DTYPE_*; the format is 1-5-2 (e5) or 1-4-3.
+int lin_split(int op, int64_t np, int64_t nq, int64_t nc, int dtype);
+void launch_lin_general(int op, int dtype, bool e5, const LinArgs& a, hipStream_t s);
+void launch_lin_join(int op, int dtype, bool e5, const LinArgs& a, hipStream_t s);
+
+}  // namespace aps
