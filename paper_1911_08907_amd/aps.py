@@ -1,6 +1,6 @@
 """Thin Python binding of libaps.so (argument marshalling only).
 
-The names match the C ABI declared in include/aps.h.  Arrays are torch tensors
+The names match the C ABI declared in include/aps.h and include/aps_linear.h.  Arrays are torch tensors
 on the GPU (torch provides device memory and the current stream); the format
 palette is a list of ``Format``.  Every computation happens in the HIP kernels
 of libaps.so; if the library is missing, loading fails loudly.
@@ -30,9 +30,10 @@ APS_MAX_FORMATS = 8
 
 EXPORTS = ("aps_format_supported", "aps_layer_maxabs", "aps_layer_scales", "aps_quantize",
            "aps_sim_reduce", "aps_sim_reduce_ex", "aps_sim_reduce_codes", "aps_dequantize", "aps_lp_gemm",
-           "aps_sync_workspace_bytes", "aps_sync_route", "aps_sync", "aps_sync_noalloc",
-           "aps_linear_workspace_bytes", "aps_linear", "aps_linear_grad_input", "aps_linear_grad_weight",
-           "aps_activation_grad", "aps_checkpoint_save", "aps_checkpoint_load", "aps_strerror")
+           "aps_sync_workspace_bytes", "aps_sync_route", "aps_sync", "aps_sync_noalloc", "aps_strerror")
+# those of include/aps_linear.h
+LINEAR_EXPORTS = ("aps_linear_workspace_bytes", "aps_linear", "aps_linear_grad_input", "aps_linear_grad_weight",
+                  "aps_activation_grad", "aps_checkpoint_save", "aps_checkpoint_load")
 
 APS_ACC_SEQUENTIAL = 0
 APS_ACC_KAHAN = 1

@@ -16,6 +16,7 @@
 #pragma once
 
 #include "aps_common.hpp"
+#include "aps_linear.h"
 
 namespace aps {
 

@@ -2,6 +2,7 @@
 reference (no GPU: every call of the library here is refused or empty)."""
 import ctypes
 import math
+import os
 
 import pytest
 import torch
@@ -10,7 +11,7 @@ import oracle as O
 from paper_1911_08907_amd import aps as A
 from paper_1911_08907_amd import build as B
 from tests import linear_ref as R
-from tests.test_abi import GOOD, MIS, no_gpu
+from tests.test_abi import GOOD, HEADER, MIS, no_gpu
 
 F43, F52 = A.Format(4, 3).c(), A.Format(5, 2).c()
 BF16, F32 = A.APS_DTYPE_BF16, A.APS_DTYPE_F32
@@ -19,10 +20,18 @@ ODD = ctypes.c_void_p(4097)
 
 @pytest.fixture(scope="module")
 def lib():
-    import os
     if not os.path.exists(A.LIB_PATH):
         B.build()
     return A.lib()
+
+
+def test_the_header_is_the_binding(lib):
+    import re
+    txt = open(os.path.join(os.path.dirname(HEADER), "aps_linear.h")).read()
+    names = set(re.findall(r"\b(aps_[a-z_]+)\s*\(", re.sub(r"/\*.*?\*/", "", txt, flags=re.S)))
+    assert names == set(A.LINEAR_EXPORTS)
+    for name in names:
+        assert hasattr(lib, name)
 
 
 def _linear(lib, **kw):
