@@ -372,4 +372,18 @@ int lin_split(int op, int64_t np, int64_t nq, int64_t nc, int dtype);
 void launch_lin_general(int op, int dtype, bool e5, const LinArgs& a, hipStream_t s);
 void launch_lin_join(int op, int dtype, bool e5, const LinArgs& a, hipStream_t s);
 
+int lin_tile_split(int64_t np, int64_t nq, int64_t nc);
+void launch_lin_tile(int op, int dtype, bool e5, const LinArgs& a, hipStream_t s);
+
 }  // namespace aps
+
+// Launch kernel K of the operator and format.
+#define APS_LIN_OPS(K, T, ...)                                                              \
+    switch (op * 2 + (e5 ? 1 : 0)) {                                                        \
+        case OP_FWD * 2: hipLaunchKernelGGL((K<T, OP_FWD, false>), __VA_ARGS__); break;     \
+        case OP_FWD * 2 + 1: hipLaunchKernelGGL((K<T, OP_FWD, true>), __VA_ARGS__); break;  \
+        case OP_DX * 2: hipLaunchKernelGGL((K<T, OP_DX, false>), __VA_ARGS__); break;       \
+        case OP_DX * 2 + 1: hipLaunchKernelGGL((K<T, OP_DX, true>), __VA_ARGS__); break;    \
+        case OP_DW * 2: hipLaunchKernelGGL((K<T, OP_DW, false>), __VA_ARGS__); break;       \
+        default: hipLaunchKernelGGL((K<T, OP_DW, true>), __VA_ARGS__); break;               \
+    }

@@ -260,15 +260,6 @@ int lin_split(int op, int64_t np, int64_t nq, int64_t nc, int dtype) {
     return (int)std::max<int64_t>(1, std::min<int64_t>(512 / tiles, nc / 128));
 }
 
-#define APS_LIN_OPS(K, T, ...)                                                              \
-    switch (op * 2 + (e5 ? 1 : 0)) {                                                        \
-        case OP_FWD * 2: hipLaunchKernelGGL((K<T, OP_FWD, false>), __VA_ARGS__); break;     \
-        case OP_FWD * 2 + 1: hipLaunchKernelGGL((K<T, OP_FWD, true>), __VA_ARGS__); break;  \
-        case OP_DX * 2: hipLaunchKernelGGL((K<T, OP_DX, false>), __VA_ARGS__); break;       \
-        case OP_DX * 2 + 1: hipLaunchKernelGGL((K<T, OP_DX, true>), __VA_ARGS__); break;    \
-        case OP_DW * 2: hipLaunchKernelGGL((K<T, OP_DW, false>), __VA_ARGS__); break;       \
-        default: hipLaunchKernelGGL((K<T, OP_DW, true>), __VA_ARGS__); break;               \
-    }
 #define APS_LIN_TYPES(K, ...)                                              \
     if (dtype == APS_DTYPE_BF16) {                                         \
         APS_LIN_OPS(K, __bf16, __VA_ARGS__)                                \

@@ -1,0 +1,373 @@
+// aps_linear_tile.hip -- the linear layer's products of 16-bit operands whose
+// rows are aligned to 16 bytes: tiles of 256 p x 256 q.
+//
+// Eight waves (two on each SIMD) form a tile, each 64 p x 128 q of it in eight
+// 32 x 32 accumulators; the contraction is staged 64 deep in two buffers of
+// LDS that the loads fill directly.  The loads of a stage are issued when the
+// previous stage starts to multiply, so one barrier per stage suffices: it
+// says both that the stage has landed and that the other buffer is read out.
+//
+// In LDS a stage lies as it does in memory, each 16-byte chunk of a row at a
+// place exclusive-ored with a few bits of the row, which the loading lane
+// chooses by the chunk it asks for:
+//   along rows   [256 rows][64 c]: a fragment is one 16-byte read per lane;
+//                chunk ^ (row / 2) & 7 gives 16 lanes 64 different banks
+//   row to row   [64 c][256 p]: a fragment is two transposing reads of 4 c x 16
+//                p per 16 lanes; chunk ^ 4 (c & 3) gives 32 lanes all banks
+//   codes        [64 c][256 p] bytes: one transposing read of 8 c x 16 p per 16
+//                lanes, chunk ^ 2 (c & 7); then four conversions of two codes,
+//                with the block's power of two, to the matrix type: exact
+// Elements past an operand's end are read as zero by the buffer loads' own
+// range check, through an offset that is out of range.
+#include "aps_linear.hpp"
+
+namespace aps {
+
+namespace {
+
+constexpr int TP = 256, TQ = 256, TK = 64;  // a workgroup's tile and stage
+constexpr int TTHREADS = 512;
+constexpr uint32_t OUT_OF_RANGE = 0x80000000u;  // as a byte offset; the loads' range ends there
+constexpr int WAIT_LOADS = 0x0F70;              // s_waitcnt vmcnt(0)
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+
+#define APS_LDS(T, p) ((__attribute__((address_space(3))) T*)(p))
+
+template <class T>
+struct Mat;
+template <>
+struct Mat<__bf16> {
+    typedef bf16x8 frag;
+    static __device__ __forceinline__ f32x16 mma(frag p, frag q, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(p, q, c, 0, 0, 0);
+    }
+    template <bool E5, bool HI>
+    static __device__ __forceinline__ uint32_t two(uint32_t w, float inv) {
+        if constexpr (E5) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, inv, HI));
+        return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, inv, HI));
+    }
+    static constexpr uint32_t INF = 0x7F80u, NAN_ = 0x7FC0u;
+    static __device__ __forceinline__ float add2(uint32_t w, float s) {
+        return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), bf16x2{(__bf16)1.0f, (__bf16)1.0f}, s, false);
+    }
+};
+template <>
+struct Mat<_Float16> {
+    typedef f16x8 frag;
+    static __device__ __forceinline__ f32x16 mma(frag p, frag q, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(p, q, c, 0, 0, 0);
+    }
+    template <bool E5, bool HI>
+    static __device__ __forceinline__ uint32_t two(uint32_t w, float inv) {
+        if constexpr (E5) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_bf8(w, inv, HI));
+        return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, inv, HI));
+    }
+    static constexpr uint32_t INF = 0x7C00u, NAN_ = 0x7E00u;
+    static __device__ __forceinline__ float add2(uint32_t w, float s) {
+        return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, w), f16x2{(_Float16)1.0f, (_Float16)1.0f}, s, false);
+    }
+};
+
+enum Kind { ALONG, ACROSS, CODES };
+
+// One operand's 256 rows (p or q): what a lane loads, and the fragments.
+template <Kind KIND>
+struct Operand {
+    static constexpr int ELEM = KIND == CODES ? 1 : 2;
+    static constexpr int BYTES = 256 * TK * ELEM;      // of a stage
+    static constexpr int LOADS = BYTES / (TTHREADS * 16);
+    const char* base;   // of the tile's first row and the stage's first c (scalar)
+    int64_t step;       // bytes from stage to stage
+    uint32_t off[LOADS];
+    int c_of;           // along: the lane's c in a stage; across: its first row c
+    int c_step;         // across: c from load to load
+
+    __device__ __forceinline__ void place(const void* p, int64_t ld, int64_t r0, int64_t nr, int64_t c0) {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        if constexpr (KIND == ALONG) {
+            base = (const char*)p + (r0 * ld + c0) * ELEM;
+            step = TK * ELEM;
+            const int chunk = (lane & 7) ^ ((4 * wave + (lane >> 4)) & 7);
+            c_of = chunk * 8;
+            c_step = 0;
+#pragma unroll
+            for (int n = 0; n < LOADS; ++n) {
+                const int row = (8 * n + wave) * 8 + (lane >> 3);
+                off[n] = r0 + row < nr ? (uint32_t)row * (uint32_t)(ld * ELEM) + chunk * 16 : OUT_OF_RANGE;
+            }
+        } else {
+            constexpr int PER_ROW = 16 * ELEM;            // chunks of a row of 256
+            constexpr int ROWS = 64 / PER_ROW;            // rows of one load
+            base = (const char*)p + (c0 * ld + r0) * ELEM;
+            step = TK * ld * ELEM;
+            const int c = ROWS * wave + lane / PER_ROW;
+            const int chunk = (lane % PER_ROW) ^ (KIND == CODES ? (c & 7) * 2 : (c & 3) * 4);
+            c_of = c;
+            c_step = 8 * ROWS;
+#pragma unroll
+            for (int n = 0; n < LOADS; ++n)
+                off[n] = r0 + chunk * (16 / ELEM) < nr
+                             ? (uint32_t)(c + n * c_step) * (uint32_t)(ld * ELEM) + chunk * 16
+                             : OUT_OF_RANGE;
+        }
+    }
+    // Stage `left` c's (64, or what is left of the contraction) into LDS.
+    __device__ __forceinline__ void load(char* lds, int64_t left) {
+        const __amdgpu_buffer_rsrc_t rsrc =
+            __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)OUT_OF_RANGE, 0x00020000);
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+        for (int n = 0; n < LOADS; ++n) {
+            uint32_t o = off[n];
+            if (left < TK) o = c_of + n * c_step < left ? o : OUT_OF_RANGE;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, APS_LDS(void, lds + (8 * n + wave) * 1024), 16, o, 0, 0, 0);
+        }
+        base += step;
+    }
+};
+
+// A wave's fragments of an operand: N of 32 rows each from row r on.  The places
+// differ from fragment to fragment and from 16 c to 16 c by constants, but for
+// the exclusive-or: along rows it depends on the 16 c, otherwise on the
+// fragment's rows.
+template <Kind KIND, int N>
+struct Reader {
+    static constexpr int BASES = KIND == ALONG ? 4 : N;
+    int at[BASES];
+    __device__ __forceinline__ void place(int r) {
+        const int lane = threadIdx.x & 63, half = lane >> 5, i = lane & 15;
+#pragma unroll
+        for (int b = 0; b < BASES; ++b) {
+            if constexpr (KIND == ALONG) {
+                const int row = lane & 31;
+                at[b] = (r + row) * 128 + ((2 * b + half) ^ ((row >> 1) & 7)) * 16;
+            } else if constexpr (KIND == ACROSS) {
+                const int c = half * 8 + (i >> 2), p = r + 32 * b + (lane & 16) + (i & 3) * 4;
+                at[b] = c * 512 + ((p >> 3) ^ ((c & 3) * 4)) * 16 + (p & 7) * 2;
+            } else {
+                const int c = half * 8 + (i >> 1), p = r + 32 * b + (lane & 16) + (i & 1) * 8;
+                at[b] = c * 256 + ((p >> 4) ^ ((c & 7) * 2)) * 16 + (p & 15);
+            }
+        }
+    }
+    // fragment n of the s-th 16 c
+    template <class T>
+    __device__ __forceinline__ typename Mat<T>::frag read(const char* lds, int n, int s) const {
+        typedef typename Mat<T>::frag F;
+        if constexpr (KIND == ALONG) return *(const F*)(lds + at[s] + n * 32 * 128);
+        const char* p = lds + at[KIND == ALONG ? 0 : n] + s * 16 * 512;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(APS_LDS(s16x4, p));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(APS_LDS(s16x4, p + 4 * 512));
+        struct { s16x4 a, b; } both = {lo, hi};
+        return __builtin_bit_cast(F, both);
+    }
+    __device__ __forceinline__ i32x2 read_codes(const char* lds, int n, int s) const {
+        return __builtin_amdgcn_ds_read_tr8_b64_v2i32(APS_LDS(i32x2, lds + at[n] + s * 16 * 256));
+    }
+};
+
+template <class T, bool E5>
+__device__ __forceinline__ typename Mat<T>::frag decode_fragment(i32x2 w, int32_t word) {
+    typedef Mat<T> M;
+    const float inv = pow2_of(-ck_ft(word));
+    u4v v = {M::template two<E5, false>(w[0], inv), M::template two<E5, true>(w[0], inv),
+             M::template two<E5, false>(w[1], inv), M::template two<E5, true>(w[1], inv)};
+    if (!E5 && (word & CK_ODD)) {  // the conversion knows no INF of 1-4-3
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t c = ((uint32_t)w[i / 4] >> (i % 4 * 8)) & 0xFFu, sh = i % 2 * 16;
+            const uint32_t x = ((c & 0x80u) << 8) | ((c & 0x7Fu) > 0x78u ? M::NAN_ : M::INF);
+            if ((c & 0x7Fu) >= 0x78u) v[i / 2] = (v[i / 2] & ~(0xFFFFu << sh)) | (x << sh);
+        }
+    }
+    return __builtin_bit_cast(typename M::frag, v);
+}
+
+template <class T, int OP, bool E5>
+__global__ __launch_bounds__(TTHREADS) void k_lin_tile(LinArgs a) {
+    constexpr Kind KP = OP == OP_FWD ? ALONG : (OP == OP_DX ? ACROSS : CODES);
+    constexpr Kind KQ = OP == OP_DW ? ACROSS : ALONG;
+    typedef Operand<KP> OpP;
+    typedef Operand<KQ> OpQ;
+    typedef typename Mat<T>::frag F;
+    __shared__ __align__(1024) char lds0[OpP::BYTES + OpQ::BYTES];
+    __shared__ __align__(1024) char lds1[OpP::BYTES + OpQ::BYTES];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wp = wave & 3, wq = wave >> 2;
+    const int64_t tp = (a.np + TP - 1) / TP, tq = (a.nq + TQ - 1) / TQ;
+    const int64_t tile = blockIdx.x % (tp * tq), piece = blockIdx.x / (tp * tq);
+    const int64_t p0 = (tile % tp) * TP, q0 = (tile / tp) * TQ;
+    const int64_t cb = piece * a.piece, ce = min(a.nc, cb + a.piece);
+
+    OpP P;
+    OpQ Q;
+    P.place(a.P, a.ldp, p0, a.np, cb);
+    Q.place(a.Q, a.ldq, q0, a.nq, cb);
+    f32x16 acc[2][4] = {};
+    // dbias: where it is asked for, the tiles of the first p sum Q's columns,
+    // each wave those of one fragment
+    const bool sums = OP == OP_DW && a.dbias && p0 == 0;
+    float sum = 0.0f;
+    Reader<KQ, 1> RS;
+    RS.place(wq * 128 + wp * 32);
+
+    Reader<KP, 2> RP;
+    Reader<KQ, 4> RQ;
+    RP.place(wp * 64);
+    RQ.place(wq * 128);
+    const int64_t nb = (a.np + CK_COLS - 1) / CK_COLS, pb = min(p0 / CK_COLS + wp / 2, nb - 1);
+
+    // one stage: the next one's loads into `fill`, the products of `use`
+    const auto load = [&](char* fill, int64_t left) {
+        P.load(fill, left);
+        Q.load(fill + OpP::BYTES, left);
+    };
+    const auto stage = [&](char* __restrict fill, const char* __restrict use, int64_t c) {
+        __builtin_amdgcn_s_waitcnt(WAIT_LOADS);
+        __syncthreads();
+        if (c + TK < ce) load(fill, ce - c - TK);
+        int32_t word[2] = {0, 0};
+        if constexpr (OP == OP_DW) {
+            word[0] = cld(a.zexps, c / CK_ROWS * nb + pb);
+            word[1] = cld(a.zexps, min(c / CK_ROWS + 1, (a.nc - 1) / CK_ROWS) * nb + pb);
+        }
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            F p[2], q[4];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                if constexpr (OP == OP_DW)
+                    p[i] = decode_fragment<T, E5>(RP.read_codes(use, i, s), word[s / 2]);
+                else
+                    p[i] = RP.template read<T>(use, i, s);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) q[j] = RQ.template read<T>(use + OpP::BYTES, j, s);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) acc[i][j] = Mat<T>::mma(p[i], q[j], acc[i][j]);
+        }
+        if (OP == OP_DW && sums) {
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                const u4v w = __builtin_bit_cast(u4v, RS.template read<T>(use + OpP::BYTES, 0, s));
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum = Mat<T>::add2(w[i], sum);
+            }
+        }
+    };
+    if (cb < ce) load(lds0, ce - cb);
+    for (int64_t c = cb; c < ce; c += 2 * TK) {
+        stage(lds1, lds0, c);
+        if (c + TK < ce) stage(lds0, lds1, c + TK);
+    }
+
+    // accumulator [i][j]: q = its lane of 32, p = 4 elements of each 8, by the lane's half
+    const int64_t ql = q0 + wq * 128 + (lane & 31), pl = p0 + wp * 64 + (lane >> 5) * 4;
+    if constexpr (OP == OP_DW) {
+        sum += __shfl_xor(sum, 32);
+        const int64_t q = ql + wp * 32;
+        if (sums && lane < 32 && q < a.nq) {
+            if (a.split > 1)
+                a.part_bias[piece * a.nq + q] = sum;
+            else
+                a.dbias[q] = a.accumulate ? a.dbias[q] + sum : sum;
+        }
+    }
+    if (a.split > 1) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int64_t q = ql + j * 32;
+            if (q >= a.nq) continue;
+            float* o = a.part + (piece * a.nq + q) * a.ldpart;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int64_t p = pl + (i / 4) * 32 + (i % 4) * 8;
+                const f32x16& v = acc[i / 4][j];
+                if (p < a.ldpart) *(f32x4*)(o + p) = f32x4{v[i % 4 * 4], v[i % 4 * 4 + 1], v[i % 4 * 4 + 2], v[i % 4 * 4 + 3]};
+            }
+        }
+        return;
+    }
+    __shared__ uint32_t red[8][4];
+    if constexpr (OP == OP_FWD) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int64_t p = pl + (i / 4) * 32 + (i % 4) * 8;
+            float b[4];
+            lin_bias4<T>(a, p, a.np - p, b);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i / 4][j][i % 4 * 4 + e] += b[e];
+        }
+        if (a.codes) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                uint32_t mx = 0;
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    if (ql + j * 32 < a.nq && pl + (i / 16) * 32 + (i % 16 / 4) * 8 + i % 4 < a.np)
+                        mx = ck_max_join(mx, ck_max_bits(ck_clamp(acc[i / 16][j][i % 16], ck_limit<T, E5>())));
+                mx = ck_wave_max(mx);
+                if (lane == 0) red[wave][j] = mx;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int32_t word = ck_word(ck_max_join(red[wave][j], red[wave ^ 1][j]), ck_emax<E5>());
+                const int64_t q = ql + j * 32, qb = (q0 + wq * 128) / CK_ROWS + j;
+                if ((wp & 1) == 0 && lane == 0 && qb * CK_ROWS < a.nq && p0 + wp * 64 < a.np) a.exps[qb * nb + pb] = word;
+                if (q >= a.nq) continue;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int64_t p = pl + (i / 4) * 32 + (i % 4) * 8;
+                    const f32x16& v = acc[i / 4][j];
+                    const float z[4] = {v[i % 4 * 4], v[i % 4 * 4 + 1], v[i % 4 * 4 + 2], v[i % 4 * 4 + 3]};
+                    lin_save4<T, E5>(a, q, p, a.np - p, ck_ft(word), z);
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int64_t q = ql + j * 32;
+        __builtin_amdgcn_sched_barrier(0);
+        if (q >= a.nq) continue;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int64_t p = pl + (i / 4) * 32 + (i % 4) * 8;
+            __builtin_amdgcn_sched_barrier(0);
+            const f32x16& v = acc[i / 4][j];
+            const float r[4] = {v[i % 4 * 4], v[i % 4 * 4 + 1], v[i % 4 * 4 + 2], v[i % 4 * 4 + 3]};
+            if (p < a.np) lin_finish4<T, OP, E5>(a, q, p, a.np - p, r);
+        }
+    }
+}
+
+}  // namespace
+
+int lin_tile_split(int64_t np, int64_t nq, int64_t nc) {
+    const int64_t tiles = ((np + TP - 1) / TP) * ((nq + TQ - 1) / TQ);
+    return (int)std::max<int64_t>(1, std::min<int64_t>(256 / tiles, nc / 256));
+}
+
+void launch_lin_tile(int op, int dtype, bool e5, const LinArgs& a, hipStream_t s) {
+    const int64_t tiles = ((a.np + TP - 1) / TP) * ((a.nq + TQ - 1) / TQ);
+    const dim3 grid((unsigned)(tiles * a.split));
+#define APS_TILE(T) APS_LIN_OPS(k_lin_tile, T, grid, dim3(TTHREADS), 0, s, a)
+    if (dtype == APS_DTYPE_BF16) {
+        APS_TILE(__bf16)
+    } else {
+        APS_TILE(_Float16)
+    }
+#undef APS_TILE
+}
+
+}  // namespace aps
