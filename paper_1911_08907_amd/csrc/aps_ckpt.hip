@@ -14,6 +14,7 @@ namespace aps {
 namespace {
 
 constexpr int CTHREADS = 256;
+constexpr int LOAD_STEPS = 2;
 
 struct CkArgs {
     const void* X;  // save: the activations; act_grad: dY
@@ -35,15 +36,23 @@ struct Walk {
     static constexpr int STEP = 64 / LANES;            // rows at a time
     static constexpr int STEPS = CK_ROWS / STEP;
     typedef T vec __attribute__((ext_vector_type(E)));
+    typedef std::conditional_t<sizeof(T) == 4, uint32_t, uint16_t> word_t;
+    typedef word_t bits __attribute__((ext_vector_type(E)));
+    static constexpr word_t MAGNITUDE = (word_t)~((word_t)1 << (8 * sizeof(T) - 1));
+    static __device__ __forceinline__ uint32_t bits_of(float v) { return __builtin_bit_cast(word_t, (T)v); }
+    static __device__ __forceinline__ float value_of(uint32_t b) { return (float)__builtin_bit_cast(T, (word_t)b); }
     int64_t row, col, have;
     int64_t block;
-    __device__ __forceinline__ bool place(const CkArgs& a) {
+    // the wave's rows of a block that `waves` waves share
+    __device__ __forceinline__ bool place(const CkArgs& a, int waves) {
         const int64_t nb = (a.C + CK_COLS - 1) / CK_COLS;
-        block = (int64_t)blockIdx.x * (CTHREADS / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        const int64_t r0 = block / nb * CK_ROWS;
+        const int64_t k = (int64_t)blockIdx.x * (CTHREADS / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int64_t rows = k / nb;  // neighbouring waves take neighbouring columns
+        const int64_t r0 = rows * (CK_ROWS / waves);
+        block = r0 / CK_ROWS * nb + k % nb;
         const int lane = threadIdx.x & 63;
         row = r0 + lane / LANES;
-        col = block % nb * CK_COLS + lane % LANES * E;
+        col = k % nb * CK_COLS + lane % LANES * E;
         have = a.C - col;
         return r0 < a.M;
     }
@@ -93,19 +102,36 @@ __global__ __launch_bounds__(CTHREADS) void k_ckpt_save(CkArgs a) {
     constexpr int E = Wk::E;
     constexpr float lim = ck_limit<T, E5>();
     Wk w;
-    if (!w.place(a)) return;
+    if (!w.place(a, 1)) return;
     typename Wk::vec x[Wk::STEPS];
 #pragma unroll
     for (int s = 0; s < Wk::STEPS; ++s) {
         const int64_t r = w.row + s * Wk::STEP;
         x[s] = load_share<T, VEC>((const T*)a.X + r * a.ldx + w.col, r < a.M ? w.have : 0);
     }
-    uint32_t mx = 0;
+    // the maximum on the magnitudes' bits, in which the values order
+    typename Wk::bits top = {};
 #pragma unroll
     for (int s = 0; s < Wk::STEPS; ++s)
+        top = __builtin_elementwise_max(top, __builtin_bit_cast(typename Wk::bits, x[s]) & Wk::MAGNITUDE);
+    uint32_t mx = 0;
 #pragma unroll
-        for (int i = 0; i < E; ++i) mx = ck_max_join(mx, ck_max_bits(ck_clamp((float)x[s][i], lim)));
-    const int32_t word = ck_word(ck_wave_max(mx), ck_emax<E5>());
+    for (int i = 0; i < E; ++i) mx = max(mx, (uint32_t)top[i]);
+#pragma unroll
+    for (int o = 32; o; o >>= 1) mx = max(mx, (uint32_t)__shfl_xor((int)mx, o));
+    mx = __builtin_amdgcn_readfirstlane(mx);
+    // INF, NaN or more than lim in the block: each element is looked at
+    const bool careful = mx > Wk::bits_of(lim);
+    mx = f2u(Wk::value_of(mx));
+    if (careful) {
+        mx = 0;
+#pragma unroll
+        for (int s = 0; s < Wk::STEPS; ++s)
+#pragma unroll
+            for (int i = 0; i < E; ++i) mx = ck_max_join(mx, ck_max_bits(ck_clamp((float)x[s][i], lim)));
+        mx = ck_wave_max(mx);
+    }
+    const int32_t word = ck_word(mx, ck_emax<E5>());
     if ((threadIdx.x & 63) == 0) a.exps[w.block] = word;
     const float up = pow2_of(ck_ft(word));
 #pragma unroll
@@ -117,7 +143,12 @@ __global__ __launch_bounds__(CTHREADS) void k_ckpt_save(CkArgs a) {
         for (int g = 0; g < E / 4; ++g) {
             float v[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = ck_clamp((float)x[s][4 * g + i], lim) * up;
+            for (int i = 0; i < 4; ++i) v[i] = (float)x[s][4 * g + i];
+            if (careful)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = ck_clamp(v[i], lim);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] *= up;
             c[g] = ck_encode4<E5>(v);
         }
         uint8_t* o = a.codes + r * a.ldc + w.col;
@@ -135,49 +166,55 @@ __global__ __launch_bounds__(CTHREADS) void k_ckpt_save(CkArgs a) {
 }
 
 // GRAD: out = X * act'(z); otherwise out = act(z), z the checkpoint's values.
+// A wave takes LOAD_STEPS of a block's steps: nothing ties the rows together,
+// and more waves hide the activations' arithmetic and a few rows' latency.
 template <class T, bool E5, bool VEC, bool GRAD>
 __global__ __launch_bounds__(CTHREADS) void k_ckpt_load(CkArgs a) {
     typedef Walk<T> Wk;
     constexpr int E = Wk::E;
     Wk w;
-    if (!w.place(a)) return;
+    if (!w.place(a, Wk::STEPS / LOAD_STEPS)) return;
     const int32_t word = a.exps[w.block];
     const float inv = pow2_of(-ck_ft(word));
-    typename CodeVec<E>::type c[Wk::STEPS];
-    typename Wk::vec x[GRAD ? Wk::STEPS : 1];
+    typename CodeVec<E>::type c[LOAD_STEPS];
+    typename Wk::vec x[GRAD ? LOAD_STEPS : 1];
 #pragma unroll
-    for (int s = 0; s < Wk::STEPS; ++s) {
+    for (int s = 0; s < LOAD_STEPS; ++s) {
         const int64_t r = w.row + s * Wk::STEP;
         const int64_t have = r < a.M ? w.have : 0;
         c[s] = load_share_codes<T, VEC>(a.codes + r * a.ldc + w.col, have);
         if constexpr (GRAD) x[s] = load_share<T, VEC>((const T*)a.X + r * a.ldx + w.col, have);
     }
+    with_act(a.act, [&](auto act) {
 #pragma unroll
-    for (int s = 0; s < Wk::STEPS; ++s) {
-        const int64_t r = w.row + s * Wk::STEP;
-        if (r >= a.M) break;
-        typename Wk::vec y;
+        for (int s = 0; s < LOAD_STEPS; ++s) {
+            const int64_t r = w.row + s * Wk::STEP;
+            if (r >= a.M) break;
+            typename Wk::vec y;
 #pragma unroll
-        for (int g = 0; g < E / 4; ++g) {
-            float z[4];
-            ck_decode4<E5>(CodeVec<E>::word(c[s], g), inv, word & CK_ODD, z);
+            for (int g = 0; g < E / 4; ++g) {
+                float z[4];
+                ck_decode4<E5>(CodeVec<E>::word(c[s], g), inv, word & CK_ODD, z);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                y[4 * g + i] = (T)(GRAD ? (float)x[GRAD ? s : 0][4 * g + i] * act_slope(z[i], a.act) : act_value(z[i], a.act));
+                for (int i = 0; i < 4; ++i)
+                    y[4 * g + i] = (T)(GRAD ? (float)x[GRAD ? s : 0][4 * g + i] * act_slope<act.value>(z[i])
+                                            : act_value<act.value>(z[i]));
+            }
+            T* o = (T*)a.out + r * a.ldo + w.col;
+            if (VEC && w.have >= E) {
+                *(typename Wk::vec*)o = y;
+            } else {
+#pragma unroll
+                for (int i = 0; i < E; ++i)
+                    if (i < w.have) o[i] = y[i];
+            }
         }
-        T* o = (T*)a.out + r * a.ldo + w.col;
-        if (VEC && w.have >= E) {
-            *(typename Wk::vec*)o = y;
-        } else {
-#pragma unroll
-            for (int i = 0; i < E; ++i)
-                if (i < w.have) o[i] = y[i];
-        }
-    }
+    });
 }
 
-dim3 grid_of(const CkArgs& a) {
-    const int64_t blocks = ((a.M + CK_ROWS - 1) / CK_ROWS) * ((a.C + CK_COLS - 1) / CK_COLS);
+// `waves` of a block
+dim3 grid_of(const CkArgs& a, int waves) {
+    const int64_t blocks = ((a.M + CK_ROWS - 1) / CK_ROWS) * ((a.C + CK_COLS - 1) / CK_COLS) * waves;
     return dim3((unsigned)((blocks + CTHREADS / 64 - 1) / (CTHREADS / 64)));
 }
 
@@ -222,7 +259,7 @@ extern "C" int aps_checkpoint_save(const void* X, int64_t ldx, int32_t M, int32_
     if (M == 0 || C == 0) return APS_OK;
     const CkArgs a{X, ldx, nullptr, 0, codes, ldc, ckpt_exp, M, C, APS_ACT_NONE};
     const bool vec = rows_of_shares(X, ldx, es, share) && rows_of_shares(codes, ldc, 1, share);
-    APS_CK_TYPES(APS_CK_SAVE, grid_of(a), dim3(CTHREADS), 0, (hipStream_t)stream, a)
+    APS_CK_TYPES(APS_CK_SAVE, grid_of(a, 1), dim3(CTHREADS), 0, (hipStream_t)stream, a)
     return launched();
 }
 
@@ -237,7 +274,7 @@ extern "C" int aps_checkpoint_load(const uint8_t* codes, int64_t ldc, const int3
     if (M == 0 || C == 0) return APS_OK;
     const CkArgs a{nullptr, 0, X, ldx, (uint8_t*)codes, ldc, (int32_t*)ckpt_exp, M, C, act};
     const bool vec = rows_of_shares(X, ldx, es, share) && rows_of_shares(codes, ldc, 1, share);
-    APS_CK_TYPES(APS_CK_LOAD, grid_of(a), dim3(CTHREADS), 0, (hipStream_t)stream, a)
+    APS_CK_TYPES(APS_CK_LOAD, grid_of(a, CK_ROWS / (64 / (CK_COLS / share)) / LOAD_STEPS), dim3(CTHREADS), 0, (hipStream_t)stream, a)
     return launched();
 }
 
@@ -255,6 +292,6 @@ extern "C" int aps_activation_grad(const void* dY, int64_t lddy, int32_t act, ap
     const CkArgs a{dY, lddy, dZ, lddz, (uint8_t*)codes, ldc, (int32_t*)ckpt_exp, M, C, act};
     const bool vec = rows_of_shares(dY, lddy, es, share) && rows_of_shares(dZ, lddz, es, share) &&
                      rows_of_shares(codes, ldc, 1, share);
-    APS_CK_TYPES(APS_CK_GRAD, grid_of(a), dim3(CTHREADS), 0, (hipStream_t)stream, a)
+    APS_CK_TYPES(APS_CK_GRAD, grid_of(a, CK_ROWS / (64 / (CK_COLS / share)) / LOAD_STEPS), dim3(CTHREADS), 0, (hipStream_t)stream, a)
     return launched();
 }

@@ -15,6 +15,8 @@
 // when it is stored in its type.
 #pragma once
 
+#include <type_traits>
+
 #include "aps_common.hpp"
 #include "aps_linear.h"
 
@@ -102,35 +104,66 @@ __device__ __forceinline__ void store_some_codes(uint8_t* p, int64_t have, bool 
 
 // ------------------------------------------------------------ activations
 //
-// The limits at +-INF are the functions' own: arguments beyond the bound,
-// where the result is exact in fp32 already, are taken at the bound, so that
-// no INF meets a zero.  NaN fails the compares and stays.
+// GELU: with h = 1 - Phi(|z|) = erfc(|z| / sqrt 2) / 2,
+//   z Phi(z) = max(z, 0) - |z| h,   Phi(z) + z phi(z) = (z < 0 ? h : 1 - h) + z phi(z)
+// so that both tails keep h's own accuracy.  erfc is Abramowitz and Stegun's
+// 7.1.26, t (a1 + ... + a5 t^4) exp(-x^2) with t = 1 / (1 + p x): its error,
+// 1.5e-7 at most, is that of a couple of fp32 roundings of Phi, and phi is the
+// same exponential.  SiLU: the logistic function by one exponential and one
+// reciprocal.  rcp and exp2 are the hardware's, off by one ulp.
+//
+// The limits at +-INF are the functions' own: the factor |z|, or z, that would
+// meet a zero is held to where the result is exact already.  NaN stays NaN.
 
-__device__ __forceinline__ float act_value(float z, int act) {
-    if (act == APS_ACT_RELU) return z < 0.0f ? 0.0f : z;
-    if (act == APS_ACT_GELU) {
-        const float c = z < -15.0f ? -15.0f : z;
-        return c * (0.5f * (1.0f + erff(c * 0.70710678118654752f)));
-    }
-    if (act == APS_ACT_SILU) {
-        const float c = z < -104.0f ? -104.0f : z;
-        return c * __builtin_amdgcn_rcpf(1.0f + expf(-c));
-    }
+struct Tail {
+    float h, e;  // 1 - Phi(|z|), exp(-z^2 / 2)
+};
+__device__ __forceinline__ Tail normal_tail(float z) {
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f * 0.70710678f, __builtin_fabsf(z), 1.0f));
+    const float e = __builtin_amdgcn_exp2f(z * z * -0.72134752f);
+    float y = __builtin_fmaf(0.5f * 1.061405429f, t, 0.5f * -1.453152027f);
+    y = __builtin_fmaf(y, t, 0.5f * 1.421413741f);
+    y = __builtin_fmaf(y, t, 0.5f * -0.284496736f);
+    y = __builtin_fmaf(y, t, 0.5f * 0.254829592f);
+    return {y * t * e, e};
+}
+__device__ __forceinline__ float logistic(float z) {
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504f));
+}
+
+template <int ACT>
+__device__ __forceinline__ float act_value(float z) {
+    if constexpr (ACT == APS_ACT_RELU) return z < 0.0f ? 0.0f : z;
+    if constexpr (ACT == APS_ACT_GELU)
+        return __builtin_fmaf(-__builtin_fminf(__builtin_fabsf(z), 15.0f), normal_tail(z).h, __builtin_fmaxf(z, 0.0f));
+    if constexpr (ACT == APS_ACT_SILU) return (z < -104.0f ? -104.0f : z) * logistic(z);
     return z;
 }
 
-__device__ __forceinline__ float act_slope(float z, int act) {
-    if (act == APS_ACT_RELU) return z > 0.0f ? 1.0f : (z != z ? z : 0.0f);
-    if (act == APS_ACT_GELU) {
-        const float c = z < -15.0f ? -15.0f : (z > 15.0f ? 15.0f : z);
-        return 0.5f * (1.0f + erff(c * 0.70710678118654752f)) + c * expf(-0.5f * c * c) * 0.39894228040143268f;
+template <int ACT>
+__device__ __forceinline__ float act_slope(float z) {
+    if constexpr (ACT == APS_ACT_RELU) return z > 0.0f ? 1.0f : (z != z ? z : 0.0f);
+    if constexpr (ACT == APS_ACT_GELU) {
+        const Tail n = normal_tail(z);
+        return __builtin_fmaf(__builtin_amdgcn_fmed3f(z, -15.0f, 15.0f), n.e * 0.39894228f, z < 0.0f ? n.h : 1.0f - n.h);
     }
-    if (act == APS_ACT_SILU) {
-        const float c = z < -104.0f ? -104.0f : (z > 104.0f ? 104.0f : z);
-        const float s = __builtin_amdgcn_rcpf(1.0f + expf(-c));
-        return s * (1.0f + c * (1.0f - s));
+    if constexpr (ACT == APS_ACT_SILU) {
+        const float s = logistic(z);
+        return s * __builtin_fmaf(__builtin_amdgcn_fmed3f(z, -104.0f, 104.0f), 1.0f - s, 1.0f);
     }
     return 1.0f;
+}
+
+// f(std::integral_constant<int, ACT>) of a call's activation: one copy of the
+// code each, chosen once.
+template <class F>
+__device__ __forceinline__ void with_act(int act, F f) {
+    switch (act) {
+        case APS_ACT_RELU: f(std::integral_constant<int, APS_ACT_RELU>()); break;
+        case APS_ACT_GELU: f(std::integral_constant<int, APS_ACT_GELU>()); break;
+        case APS_ACT_SILU: f(std::integral_constant<int, APS_ACT_SILU>()); break;
+        default: f(std::integral_constant<int, APS_ACT_NONE>()); break;
+    }
 }
 
 // ------------------------------------------------------------ checkpoints
@@ -254,44 +287,77 @@ __device__ __forceinline__ uint32_t ck_wave_max(uint32_t m) {
     return m;
 }
 
-// The stored result of four consecutive p of row q (the first `have` of them),
+// What the epilogue reads besides the sums, for N consecutive p of row q.
+template <class T, int OP, int N>
+struct LinRead {
+    typedef T t4 __attribute__((ext_vector_type(4)));
+    t4 r[OP == OP_DW ? 1 : N / 4];
+    uint32_t c[OP == OP_DX ? N / 4 : 1];
+    int32_t word;
+    static __device__ __forceinline__ t4 load_raw(const T* s, int64_t have, bool vec) {
+        if (vec && have >= 4) return *(const t4*)s;
+        t4 v = {};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < have) v[i] = s[i];
+        return v;
+    }
+    // the first `have` of the N; p within one block of columns
+    __device__ __forceinline__ void read(const LinArgs& a, int64_t q, int64_t p, int64_t have) {
+        if constexpr (OP != OP_DW) {
+            if (a.R)
+#pragma unroll
+                for (int i = 0; i < N; i += 4) r[i / 4] = load_raw((const T*)a.R + q * a.ldr + p + i, have - i, a.vec & LV_R);
+        }
+        if constexpr (OP == OP_DX) {
+            word = 0;
+            if (a.zc) {
+#pragma unroll
+                for (int i = 0; i < N; i += 4) c[i / 4] = load_codes4(a.zc + q * a.ldzc + p + i, have - i, a.vec & LV_ZC);
+                if (have > 0) word = a.zexps[(q / CK_ROWS) * ((a.np + CK_COLS - 1) / CK_COLS) + p / CK_COLS];
+            }
+        }
+    }
+};
+
+// The stored result of N consecutive p of row q (the first `have` of them),
 // v being the finished sums: bias already added in the forward pass.
-template <class T, int OP, bool E5>
-__device__ __forceinline__ void lin_finish4(const LinArgs& a, int64_t q, int64_t p, int64_t have, const float v[4]) {
-    float y[4];
-    if constexpr (OP == OP_DW) {
-        float* o = (float*)a.out + q * a.ldo + p;
-        if (a.accumulate) {
-            load_some(o, have, a.vec & LV_OUT, y);
+template <class T, int OP, bool E5, int N, int ACT>
+__device__ __forceinline__ void lin_finish(const LinArgs& a, const LinRead<T, OP, N>& in, int64_t q, int64_t p, int64_t have,
+                                           const float v[N]) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) y[i] += v[i];
-            store_some(o, have, a.vec & LV_OUT, y);
-        } else {
-            store_some(o, have, a.vec & LV_OUT, v);
+    for (int i = 0; i < N; i += 4) {
+        float y[4];
+        if constexpr (OP == OP_DW) {
+            float* o = (float*)a.out + q * a.ldo + p + i;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = 0.0f;
+            if (a.accumulate) load_some(o, have - i, a.vec & LV_OUT, y);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = a.accumulate ? y[e] + v[i + e] : v[i + e];
+            store_some(o, have - i, a.vec & LV_OUT, y);
+            continue;
         }
-        return;
-    }
-    if constexpr (OP == OP_FWD) {
+        if constexpr (OP == OP_FWD) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] = act_value(v[i], a.act);
-    } else {
+            for (int e = 0; e < 4; ++e) y[e] = act_value<ACT>(v[i + e]);
+        } else if constexpr (OP == OP_DX) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] = v[i];
-        if (a.zc) {
-            const int32_t word = a.zexps[(q / CK_ROWS) * ((a.np + CK_COLS - 1) / CK_COLS) + p / CK_COLS];
-            float z[4];
-            ck_decode4<E5>(load_codes4(a.zc + q * a.ldzc + p, have, a.vec & LV_ZC), pow2_of(-ck_ft(word)), word & CK_ODD, z);
+            for (int e = 0; e < 4; ++e) y[e] = v[i + e];
+            if constexpr (ACT != APS_ACT_NONE) {
+                float z[4];
+                ck_decode4<E5>(in.c[i / 4], pow2_of(-ck_ft(in.word)), in.word & CK_ODD, z);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) y[i] *= act_slope(z[i], a.act);
+                for (int e = 0; e < 4; ++e) y[e] *= act_slope<ACT>(z[e]);
+            }
+        }
+        if constexpr (OP != OP_DW) {
+            if (a.R)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[e] += (float)in.r[i / 4][e];
+            store_some((T*)a.out + q * a.ldo + p + i, have - i, a.vec & LV_OUT, y);
         }
     }
-    if (a.R) {
-        float r[4];
-        load_some((const T*)a.R + q * a.ldr + p, have, a.vec & LV_R, r);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] += r[i];
-    }
-    store_some((T*)a.out + q * a.ldo + p, have, a.vec & LV_OUT, y);
 }
 
 template <class T>

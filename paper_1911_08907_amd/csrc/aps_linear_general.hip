@@ -187,13 +187,18 @@ __global__ __launch_bounds__(GTHREADS) void k_lin_general(LinArgs a) {
         }
     }
     if (q < a.nq)
+        with_act(OP == OP_DW ? APS_ACT_NONE : a.act, [&](auto act) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int64_t p = pl + 8 * i;
-            const float v[4] = {acc[i / 4][i % 4 * 4], acc[i / 4][i % 4 * 4 + 1], acc[i / 4][i % 4 * 4 + 2],
-                                acc[i / 4][i % 4 * 4 + 3]};
-            if (p < a.np) lin_finish4<T, OP, E5>(a, q, p, a.np - p, v);
-        }
+            for (int i = 0; i < 8; ++i) {
+                const int64_t p = pl + 8 * i;
+                const float v[4] = {acc[i / 4][i % 4 * 4], acc[i / 4][i % 4 * 4 + 1], acc[i / 4][i % 4 * 4 + 2],
+                                    acc[i / 4][i % 4 * 4 + 3]};
+                if (p >= a.np) break;
+                LinRead<T, OP, 4> in;
+                in.read(a, q, p, a.np - p);
+                lin_finish<T, OP, E5, 4, act.value>(a, in, q, p, a.np - p, v);
+            }
+        });
 }
 
 // The sum of a split contraction's pieces, in their order, and the epilogue:
@@ -241,13 +246,17 @@ __global__ __launch_bounds__(GTHREADS) void k_lin_join(LinArgs a) {
         if (threadIdx.x == 0) a.exps[qb * tp + pb] = word;
     }
     if (have <= 0) return;
+    with_act(OP == OP_DW ? APS_ACT_NONE : a.act, [&](auto act) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int64_t q = q0 + 8 * j;
-        if (q >= a.nq) break;
-        if (OP == OP_FWD && a.codes) lin_save4<T, E5>(a, q, p, have, ck_ft(word), v[j]);
-        lin_finish4<T, OP, E5>(a, q, p, have, v[j]);
-    }
+        for (int j = 0; j < 4; ++j) {
+            const int64_t q = q0 + 8 * j;
+            if (q >= a.nq) break;
+            if (OP == OP_FWD && a.codes) lin_save4<T, E5>(a, q, p, have, ck_ft(word), v[j]);
+            LinRead<T, OP, 4> in;
+            in.read(a, q, p, have);
+            lin_finish<T, OP, E5, 4, act.value>(a, in, q, p, have, v[j]);
+        }
+    });
 }
 
 }  // namespace

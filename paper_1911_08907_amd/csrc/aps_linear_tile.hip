@@ -27,6 +27,8 @@ namespace {
 
 constexpr int TP = 256, TQ = 256, TK = 64;  // a workgroup's tile and stage
 constexpr int TTHREADS = 512;
+constexpr int TURN_BYTES = 64 * 64 * 4;         // a wave's part of the epilogue
+constexpr int STAGE_BYTES = 4 * TURN_BYTES;     // one of the two buffers: four waves' parts, and at least a stage
 constexpr uint32_t OUT_OF_RANGE = 0x80000000u;  // as a byte offset; the loads' range ends there
 constexpr int WAIT_LOADS = 0x0F70;              // s_waitcnt vmcnt(0)
 
@@ -187,6 +189,21 @@ __device__ __forceinline__ typename Mat<T>::frag decode_fragment(i32x2 w, int32_
     return __builtin_bit_cast(typename M::frag, v);
 }
 
+// Which tile and piece a workgroup forms.  Workgroups go to the eight XCDs in
+// turn, each with an L2 of its own: an XCD takes a run of consecutive tiles,
+// and consecutive tiles fill strips of four q by all p, so that those at work
+// at a time share their operands' rows.
+struct TilePlace {
+    int64_t p, q, piece;
+};
+__device__ __forceinline__ TilePlace tile_place(int64_t tp, int64_t tq) {
+    const int64_t n = gridDim.x, b = blockIdx.x, xcd = b % 8, each = n / 8, more = n % 8;
+    const int64_t k = xcd * each + min(xcd, more) + b / 8;
+    const int64_t t = k % (tp * tq), strip = t / (4 * tp), first = strip * 4, high = min(tq - first, (int64_t)4);
+    const int64_t in = t - strip * 4 * tp;
+    return {in / high, first + in % high, k / (tp * tq)};
+}
+
 template <class T, int OP, bool E5>
 __global__ __launch_bounds__(TTHREADS) void k_lin_tile(LinArgs a) {
     constexpr Kind KP = OP == OP_FWD ? ALONG : (OP == OP_DX ? ACROSS : CODES);
@@ -194,21 +211,38 @@ __global__ __launch_bounds__(TTHREADS) void k_lin_tile(LinArgs a) {
     typedef Operand<KP> OpP;
     typedef Operand<KQ> OpQ;
     typedef typename Mat<T>::frag F;
-    __shared__ __align__(1024) char lds0[OpP::BYTES + OpQ::BYTES];
-    __shared__ __align__(1024) char lds1[OpP::BYTES + OpQ::BYTES];
+    static_assert(OpP::BYTES + OpQ::BYTES <= STAGE_BYTES, "a stage fits its buffer");
+    __shared__ __align__(1024) char lds0[STAGE_BYTES];
+    __shared__ __align__(1024) char lds1[STAGE_BYTES];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wp = wave & 3, wq = wave >> 2;
-    const int64_t tp = (a.np + TP - 1) / TP, tq = (a.nq + TQ - 1) / TQ;
-    const int64_t tile = blockIdx.x % (tp * tq), piece = blockIdx.x / (tp * tq);
-    const int64_t p0 = (tile % tp) * TP, q0 = (tile / tp) * TQ;
+    const TilePlace at = tile_place((a.np + TP - 1) / TP, (a.nq + TQ - 1) / TQ);
+    const int64_t p0 = at.p * TP, q0 = at.q * TQ, piece = at.piece;
     const int64_t cb = piece * a.piece, ce = min(a.nc, cb + a.piece);
 
     OpP P;
     OpQ Q;
     P.place(a.P, a.ldp, p0, a.np, cb);
     Q.place(a.Q, a.ldq, q0, a.nq, cb);
-    f32x16 acc[2][4] = {};
+    // the sums begin with the bias: p = 32 i + 8 g + 4 (lane / 32) + e of
+    // accumulator i's element 4 g + e
+    f32x16 acc[2][4];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        f32x16 b = {};
+        if (OP == OP_FWD && a.split == 1 && a.bias)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int64_t p = p0 + wp * 64 + i * 32 + g * 8 + (lane >> 5) * 4;
+                float v[4];
+                lin_bias4<T>(a, p, a.np - p, v);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) b[4 * g + e] = v[e];
+            }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = b;
+    }
     // dbias: where it is asked for, the tiles of the first p sum Q's columns,
     // each wave those of one fragment
     const bool sums = OP == OP_DW && a.dbias && p0 == 0;
@@ -269,10 +303,10 @@ __global__ __launch_bounds__(TTHREADS) void k_lin_tile(LinArgs a) {
     }
 
     // accumulator [i][j]: q = its lane of 32, p = 4 elements of each 8, by the lane's half
-    const int64_t ql = q0 + wq * 128 + (lane & 31), pl = p0 + wp * 64 + (lane >> 5) * 4;
+    const int64_t ql = q0 + wq * 128;
     if constexpr (OP == OP_DW) {
         sum += __shfl_xor(sum, 32);
-        const int64_t q = ql + wp * 32;
+        const int64_t q = ql + wp * 32 + lane;
         if (sums && lane < 32 && q < a.nq) {
             if (a.split > 1)
                 a.part_bias[piece * a.nq + q] = sum;
@@ -280,75 +314,96 @@ __global__ __launch_bounds__(TTHREADS) void k_lin_tile(LinArgs a) {
                 a.dbias[q] = a.accumulate ? a.dbias[q] + sum : sum;
         }
     }
-    if (a.split > 1) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int64_t q = ql + j * 32;
-            if (q >= a.nq) continue;
-            float* o = a.part + (piece * a.nq + q) * a.ldpart;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int64_t p = pl + (i / 4) * 32 + (i % 4) * 8;
-                const f32x16& v = acc[i / 4][j];
-                if (p < a.ldpart) *(f32x4*)(o + p) = f32x4{v[i % 4 * 4], v[i % 4 * 4 + 1], v[i % 4 * 4 + 2], v[i % 4 * 4 + 3]};
-            }
-        }
-        return;
-    }
-    __shared__ uint32_t red[8][4];
+    __syncthreads();  // the stages are read out
+    int32_t word[4] = {0, 0, 0, 0};
     if constexpr (OP == OP_FWD) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int64_t p = pl + (i / 4) * 32 + (i % 4) * 8;
-            float b[4];
-            lin_bias4<T>(a, p, a.np - p, b);
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[i / 4][j][i % 4 * 4 + e] += b[e];
-        }
         if (a.codes) {
+            // a block of 32 q x 128 p is two waves': its maximum goes by LDS
+            uint32_t* red = (uint32_t*)lds0;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                uint32_t mx = 0;
+                float m = 0.0f, bad = 0.0f;
 #pragma unroll
-                for (int i = 0; i < 32; ++i)
-                    if (ql + j * 32 < a.nq && pl + (i / 16) * 32 + (i % 16 / 4) * 8 + i % 4 < a.np)
-                        mx = ck_max_join(mx, ck_max_bits(ck_clamp(acc[i / 16][j][i % 16], ck_limit<T, E5>())));
-                mx = ck_wave_max(mx);
-                if (lane == 0) red[wave][j] = mx;
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        m = __builtin_fmaxf(m, __builtin_fabsf(acc[i][j][e]));
+                        bad = __builtin_fmaf(acc[i][j][e], 0.0f, bad);
+                    }
+                uint32_t mx = f2u(__builtin_fminf(m, ck_limit<T, E5>()));
+                if (bad != 0.0f) {  // an INF or NaN: the maximum of the others
+                    mx = 0;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            mx = ck_max_join(mx, ck_max_bits(ck_clamp(acc[i][j][e], ck_limit<T, E5>())));
+                }
+                mx = ck_wave_max(ql + j * 32 + (lane & 31) < a.nq ? mx : 0);
+                if (lane == 0) red[wave * 4 + j] = mx;
             }
             __syncthreads();
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int32_t word = ck_word(ck_max_join(red[wave][j], red[wave ^ 1][j]), ck_emax<E5>());
-                const int64_t q = ql + j * 32, qb = (q0 + wq * 128) / CK_ROWS + j;
-                if ((wp & 1) == 0 && lane == 0 && qb * CK_ROWS < a.nq && p0 + wp * 64 < a.np) a.exps[qb * nb + pb] = word;
-                if (q >= a.nq) continue;
+                word[j] = ck_word(ck_max_join(red[wave * 4 + j], red[(wave ^ 1) * 4 + j]), ck_emax<E5>());
+                const int64_t qb = ql / CK_ROWS + j;
+                if ((wp & 1) == 0 && lane == 0 && qb * CK_ROWS < a.nq && p0 + wp * 64 < a.np)
+                    a.exps[qb * nb + p0 / CK_COLS + wp / 2] = word[j];
+            }
+            __syncthreads();
+        }
+    }
+    // Each wave turns its accumulators through 16 KB of LDS of its own, 64 q x
+    // 64 p at a time, so that eight lanes store a row's 64 p; a 16-byte chunk
+    // of row q lies at chunk ^ q & 15.
+    char* turn = (wave < 4 ? lds0 : lds1) + (wave & 3) * TURN_BYTES;
+    const int64_t p = p0 + wp * 64 + (lane & 7) * 8, have = a.np - p;
+    with_act(OP == OP_DW || a.split > 1 ? APS_ACT_NONE : a.act, [&](auto act) {
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            const int64_t qr = ql + r * 64;
+            if (qr >= a.nq) break;
+            LinRead<T, OP, 8> in[8];
+            if (a.split == 1)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const int64_t q = qr + k * 8 + (lane >> 3);
+                    in[k].read(a, q, p, q < a.nq ? have : 0);
+                }
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const int64_t p = pl + (i / 4) * 32 + (i % 4) * 8;
-                    const f32x16& v = acc[i / 4][j];
-                    const float z[4] = {v[i % 4 * 4], v[i % 4 * 4 + 1], v[i % 4 * 4 + 2], v[i % 4 * 4 + 3]};
-                    lin_save4<T, E5>(a, q, p, a.np - p, ck_ft(word), z);
+                    const f32x16& v = acc[i / 4][2 * r + j];
+                    const int row = j * 32 + (lane & 31), chunk = (i / 4) * 8 + (i % 4) * 2 + (lane >> 5);
+                    *(f32x4*)(turn + row * 256 + (chunk ^ (row & 15)) * 16) =
+                        f32x4{v[i % 4 * 4], v[i % 4 * 4 + 1], v[i % 4 * 4 + 2], v[i % 4 * 4 + 3]};
                 }
+            wave_lds_sync();
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int row = k * 8 + (lane >> 3);
+                const int64_t q = qr + row;
+                const f32x4 lo = *(const f32x4*)(turn + row * 256 + (((lane & 7) * 2) ^ (row & 15)) * 16);
+                const f32x4 hi = *(const f32x4*)(turn + row * 256 + (((lane & 7) * 2 + 1) ^ (row & 15)) * 16);
+                const float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+                if (q >= a.nq || have <= 0) continue;
+                if (a.split > 1) {
+                    float* o = a.part + (piece * a.nq + q) * a.ldpart + p;  // ldpart is a multiple of 4
+                    *(f32x4*)o = lo;
+                    if (have > 4) *(f32x4*)(o + 4) = hi;
+                    continue;
+                }
+                if (OP == OP_FWD && a.codes) {
+                    const int ft = ck_ft(word[2 * r + k / 4]);
+                    lin_save4<T, E5>(a, q, p, have, ft, v);
+                    lin_save4<T, E5>(a, q, p + 4, have - 4, ft, v + 4);
+                }
+                lin_finish<T, OP, E5, 8, act.value>(a, in[k], q, p, have, v);
             }
+            wave_lds_sync();
         }
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int64_t q = ql + j * 32;
-        __builtin_amdgcn_sched_barrier(0);
-        if (q >= a.nq) continue;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int64_t p = pl + (i / 4) * 32 + (i % 4) * 8;
-            __builtin_amdgcn_sched_barrier(0);
-            const f32x16& v = acc[i / 4][j];
-            const float r[4] = {v[i % 4 * 4], v[i % 4 * 4 + 1], v[i % 4 * 4 + 2], v[i % 4 * 4 + 3]};
-            if (p < a.np) lin_finish4<T, OP, E5>(a, q, p, a.np - p, r);
-        }
-    }
+    });
 }
 
 }  // namespace
