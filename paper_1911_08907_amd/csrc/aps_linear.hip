@@ -23,14 +23,17 @@ int64_t part_stride(int64_t np) { return (np + 3) / 4 * 4; }
 enum Kernel { GENERAL, TILE };
 struct Plan {
     Kernel kernel;
-    int split;
+    int shape, split;
 };
 
 // `fast`: the operands' rows are aligned for the tile kernel.
 Plan plan_of(int op, const Dims& d, int dtype, bool fast) {
-    if (d.np == 0 || d.nq == 0) return {GENERAL, 1};
-    if (fast && dtype != APS_DTYPE_F32 && d.np >= 128 && d.nq >= 128) return {TILE, lin_tile_split(d.np, d.nq, d.nc)};
-    return {GENERAL, lin_split(op, d.np, d.nq, d.nc, dtype)};
+    if (d.np == 0 || d.nq == 0) return {GENERAL, 0, 1};
+    if (fast && dtype != APS_DTYPE_F32) {
+        const LinTile t = lin_tile(d.np, d.nq, d.nc);
+        return {TILE, t.shape, t.split};
+    }
+    return {GENERAL, 0, lin_split(op, d.np, d.nq, d.nc, dtype)};
 }
 
 uint64_t workspace_of(int op, const Dims& d, int dtype) {
@@ -52,7 +55,7 @@ int launch_product(int op, int dtype, bool e5, LinArgs& a, void* workspace, hipS
         a.part_bias = a.part + a.split * a.nq * a.ldpart;
     }
     if (plan.kernel == TILE)
-        launch_lin_tile(op, dtype, e5, a, s);
+        launch_lin_tile(op, dtype, e5, plan.shape, a, s);
     else
         launch_lin_general(op, dtype, e5, a, s);
     if (a.split > 1) launch_lin_join(op, dtype, e5, a, s);

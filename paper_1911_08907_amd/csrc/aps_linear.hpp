@@ -438,8 +438,13 @@ int lin_split(int op, int64_t np, int64_t nq, int64_t nc, int dtype);
 void launch_lin_general(int op, int dtype, bool e5, const LinArgs& a, hipStream_t s);
 void launch_lin_join(int op, int dtype, bool e5, const LinArgs& a, hipStream_t s);
 
-int lin_tile_split(int64_t np, int64_t nq, int64_t nc);
-void launch_lin_tile(int op, int dtype, bool e5, const LinArgs& a, hipStream_t s);
+// The tile kernel's shapes, and its choice for an output and a contraction.
+enum LinShape : int32_t { LIN_BIG, LIN_MIDDLE, LIN_SMALL };
+struct LinTile {
+    int shape, split;
+};
+LinTile lin_tile(int64_t np, int64_t nq, int64_t nc);
+void launch_lin_tile(int op, int dtype, bool e5, int shape, const LinArgs& a, hipStream_t s);
 
 }  // namespace aps
 

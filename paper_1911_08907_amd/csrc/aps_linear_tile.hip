@@ -1,22 +1,25 @@
 // aps_linear_tile.hip -- the linear layer's products of 16-bit operands whose
-// rows are aligned to 16 bytes: tiles of 256 p x 256 q.
+// rows are aligned to 16 bytes.
 //
-// Eight waves (two on each SIMD) form a tile, each 64 p x 128 q of it in eight
-// 32 x 32 accumulators; the contraction is staged 64 deep in two buffers of
-// LDS that the loads fill directly.  The loads of a stage are issued when the
-// previous stage starts to multiply, so one barrier per stage suffices: it
+// A workgroup forms a tile of 256 p x 256 q with eight waves (two on each
+// SIMD), 128 x 128 with four, or 128 x 64 with four; each wave two by four, two
+// or one 32 x 32 accumulators.  The contraction is staged 64 deep in two
+// buffers of LDS that the loads fill directly.  A stage's loads are issued
+// in the first half of the stage before, so one barrier per stage suffices: it
 // says both that the stage has landed and that the other buffer is read out.
+// Within a stage a fragment is read one step of 16 c before its products.
 //
 // In LDS a stage lies as it does in memory, each 16-byte chunk of a row at a
 // place exclusive-ored with a few bits of the row, which the loading lane
 // chooses by the chunk it asks for:
-//   along rows   [256 rows][64 c]: a fragment is one 16-byte read per lane;
+//   along rows   [rows][64 c]: a fragment is one 16-byte read per lane;
 //                chunk ^ (row / 2) & 7 gives 16 lanes 64 different banks
-//   row to row   [64 c][256 p]: a fragment is two transposing reads of 4 c x 16
-//                p per 16 lanes; chunk ^ 4 (c & 3) gives 32 lanes all banks
-//   codes        [64 c][256 p] bytes: one transposing read of 8 c x 16 p per 16
-//                lanes, chunk ^ 2 (c & 7); then four conversions of two codes,
-//                with the block's power of two, to the matrix type: exact
+//   row to row   [64 c][p]: a fragment is two transposing reads of 4 c x 16 p
+//                per 16 lanes; chunk ^ 4 (c & 3) gives 32 lanes all banks
+//   codes        [64 c][p] bytes: one transposing read of 8 c x 16 p per 16
+//                lanes, chunk ^ 2 (c & 7) (rows of 256; half of that for 128);
+//                then four conversions of two codes, with the block's power of
+//                two, to the matrix type: exact
 // Elements past an operand's end are read as zero by the buffer loads' own
 // range check, through an offset that is out of range.
 #include "aps_linear.hpp"
@@ -25,10 +28,18 @@ namespace aps {
 
 namespace {
 
-constexpr int TP = 256, TQ = 256, TK = 64;  // a workgroup's tile and stage
-constexpr int TTHREADS = 512;
-constexpr int TURN_BYTES = 64 * 64 * 4;         // a wave's part of the epilogue
-constexpr int STAGE_BYTES = 4 * TURN_BYTES;     // one of the two buffers: four waves' parts, and at least a stage
+constexpr int TK = 64;  // contraction elements of a stage
+
+// FQ accumulators of 32 q by two of 32 p a wave, WP x WQ waves.
+template <int FQ_, int WP_, int WQ_>
+struct Shape {
+    static constexpr int FQ = FQ_, WP = WP_, WQ = WQ_;
+    static constexpr int WAVES = WP * WQ, THREADS = 64 * WAVES, TP = 64 * WP, TQ = 32 * FQ * WQ;
+};
+typedef Shape<4, 4, 2> Big;     // 256 p x 256 q
+typedef Shape<2, 2, 2> Middle;  // 128 x 128
+typedef Shape<1, 2, 2> Small;   // 128 x 64
+
 constexpr uint32_t OUT_OF_RANGE = 0x80000000u;  // as a byte offset; the loads' range ends there
 constexpr int WAIT_LOADS = 0x0F70;              // s_waitcnt vmcnt(0)
 
@@ -76,12 +87,23 @@ struct Mat<_Float16> {
 
 enum Kind { ALONG, ACROSS, CODES };
 
-// One operand's 256 rows (p or q): what a lane loads, and the fragments.
-template <Kind KIND>
+// What the place of a row-to-row operand's chunk is exclusive-ored with, in
+// chunks: R elements of ELEM bytes a row.  Rows shorter than the 256 bytes of
+// the banks take turns by themselves.
+template <int R, int ELEM>
+__device__ __forceinline__ int across_xor(int c) {
+    constexpr int PER = 256 / (R * ELEM) > 1 ? 256 / (R * ELEM) : 1;  // rows of 256 bytes
+    if constexpr (ELEM == 1) return (c / PER & (8 / PER - 1)) * 2;
+    return (c / PER & (4 / PER - 1)) * 4;
+}
+
+// One operand's R rows (p or q): what a lane loads.
+template <Kind KIND, int R, int WAVES>
 struct Operand {
     static constexpr int ELEM = KIND == CODES ? 1 : 2;
-    static constexpr int BYTES = 256 * TK * ELEM;      // of a stage
-    static constexpr int LOADS = BYTES / (TTHREADS * 16);
+    static constexpr int BYTES = R * TK * ELEM;  // of a stage
+    static constexpr int LOADS = BYTES / (WAVES * 1024);
+    static_assert(LOADS * WAVES * 1024 == BYTES, "whole loads of every wave");
     const char* base;   // of the tile's first row and the stage's first c (scalar)
     int64_t step;       // bytes from stage to stage
     uint32_t off[LOADS];
@@ -98,18 +120,19 @@ struct Operand {
             c_step = 0;
 #pragma unroll
             for (int n = 0; n < LOADS; ++n) {
-                const int row = (8 * n + wave) * 8 + (lane >> 3);
+                const int row = (WAVES * n + wave) * 8 + (lane >> 3);
                 off[n] = r0 + row < nr ? (uint32_t)row * (uint32_t)(ld * ELEM) + chunk * 16 : OUT_OF_RANGE;
             }
         } else {
-            constexpr int PER_ROW = 16 * ELEM;            // chunks of a row of 256
+            constexpr int PER_ROW = R * ELEM / 16;        // chunks of a row
             constexpr int ROWS = 64 / PER_ROW;            // rows of one load
+            static_assert(WAVES * ROWS % 8 == 0, "the exclusive-or is the same for each of a lane's loads");
             base = (const char*)p + (c0 * ld + r0) * ELEM;
             step = TK * ld * ELEM;
             const int c = ROWS * wave + lane / PER_ROW;
-            const int chunk = (lane % PER_ROW) ^ (KIND == CODES ? (c & 7) * 2 : (c & 3) * 4);
+            const int chunk = (lane % PER_ROW) ^ across_xor<R, ELEM>(c);
             c_of = c;
-            c_step = 8 * ROWS;
+            c_step = WAVES * ROWS;
 #pragma unroll
             for (int n = 0; n < LOADS; ++n)
                 off[n] = r0 + chunk * (16 / ELEM) < nr
@@ -117,26 +140,23 @@ struct Operand {
                              : OUT_OF_RANGE;
         }
     }
-    // Stage `left` c's (64, or what is left of the contraction) into LDS.
-    __device__ __forceinline__ void load(char* lds, int64_t left) {
+    // The n-th load of a stage with `left` c's (at least 64 but at the end of
+    // the contraction, none or fewer after it) into LDS.
+    __device__ __forceinline__ void load(char* lds, int n, int left) const {
         const __amdgpu_buffer_rsrc_t rsrc =
             __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)OUT_OF_RANGE, 0x00020000);
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-#pragma unroll
-        for (int n = 0; n < LOADS; ++n) {
-            uint32_t o = off[n];
-            if (left < TK) o = c_of + n * c_step < left ? o : OUT_OF_RANGE;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, APS_LDS(void, lds + (8 * n + wave) * 1024), 16, o, 0, 0, 0);
-        }
-        base += step;
+        const uint32_t o = c_of + n * c_step < left ? off[n] : OUT_OF_RANGE;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, APS_LDS(void, lds + (WAVES * n + wave) * 1024), 16, o, 0, 0, 0);
     }
+    __device__ __forceinline__ void next() { base += step; }
 };
 
 // A wave's fragments of an operand: N of 32 rows each from row r on.  The places
 // differ from fragment to fragment and from 16 c to 16 c by constants, but for
 // the exclusive-or: along rows it depends on the 16 c, otherwise on the
 // fragment's rows.
-template <Kind KIND, int N>
+template <Kind KIND, int R, int N>
 struct Reader {
     static constexpr int BASES = KIND == ALONG ? 4 : N;
     int at[BASES];
@@ -149,10 +169,10 @@ struct Reader {
                 at[b] = (r + row) * 128 + ((2 * b + half) ^ ((row >> 1) & 7)) * 16;
             } else if constexpr (KIND == ACROSS) {
                 const int c = half * 8 + (i >> 2), p = r + 32 * b + (lane & 16) + (i & 3) * 4;
-                at[b] = c * 512 + ((p >> 3) ^ ((c & 3) * 4)) * 16 + (p & 7) * 2;
+                at[b] = c * (2 * R) + ((p >> 3) ^ across_xor<R, 2>(c)) * 16 + (p & 7) * 2;
             } else {
                 const int c = half * 8 + (i >> 1), p = r + 32 * b + (lane & 16) + (i & 1) * 8;
-                at[b] = c * 256 + ((p >> 4) ^ ((c & 7) * 2)) * 16 + (p & 15);
+                at[b] = c * R + ((p >> 4) ^ across_xor<R, 1>(c)) * 16 + (p & 15);
             }
         }
     }
@@ -161,14 +181,14 @@ struct Reader {
     __device__ __forceinline__ typename Mat<T>::frag read(const char* lds, int n, int s) const {
         typedef typename Mat<T>::frag F;
         if constexpr (KIND == ALONG) return *(const F*)(lds + at[s] + n * 32 * 128);
-        const char* p = lds + at[KIND == ALONG ? 0 : n] + s * 16 * 512;
+        const char* p = lds + at[KIND == ALONG ? 0 : n] + s * 16 * (2 * R);
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(APS_LDS(s16x4, p));
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(APS_LDS(s16x4, p + 4 * 512));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(APS_LDS(s16x4, p + 4 * (2 * R)));
         struct { s16x4 a, b; } both = {lo, hi};
         return __builtin_bit_cast(F, both);
     }
     __device__ __forceinline__ i32x2 read_codes(const char* lds, int n, int s) const {
-        return __builtin_amdgcn_ds_read_tr8_b64_v2i32(APS_LDS(i32x2, lds + at[n] + s * 16 * 256));
+        return __builtin_amdgcn_ds_read_tr8_b64_v2i32(APS_LDS(i32x2, lds + at[n] + s * 16 * R));
     }
 };
 
@@ -204,22 +224,25 @@ __device__ __forceinline__ TilePlace tile_place(int64_t tp, int64_t tq) {
     return {in / high, first + in % high, k / (tp * tq)};
 }
 
-template <class T, int OP, bool E5>
-__global__ __launch_bounds__(TTHREADS) void k_lin_tile(LinArgs a) {
+template <class T, int OP, bool E5, class S>
+__global__ __launch_bounds__(S::THREADS, 2) void k_lin_tile(LinArgs a) {
+    constexpr int FQ = S::FQ, WP = S::WP, TP = S::TP, TQ = S::TQ;
     constexpr Kind KP = OP == OP_FWD ? ALONG : (OP == OP_DX ? ACROSS : CODES);
     constexpr Kind KQ = OP == OP_DW ? ACROSS : ALONG;
-    typedef Operand<KP> OpP;
-    typedef Operand<KQ> OpQ;
+    typedef Operand<KP, TP, S::WAVES> OpP;
+    typedef Operand<KQ, TQ, S::WAVES> OpQ;
     typedef typename Mat<T>::frag F;
-    static_assert(OpP::BYTES + OpQ::BYTES <= STAGE_BYTES, "a stage fits its buffer");
-    __shared__ __align__(1024) char lds0[STAGE_BYTES];
-    __shared__ __align__(1024) char lds1[STAGE_BYTES];
+    // the epilogue turns a wave's accumulators through LDS, RF of its FQ at a time
+    constexpr int RF = FQ < 2 ? FQ : 2, TURN = RF * 32 * 64 * 4;
+    constexpr int STAGE = std::max(OpP::BYTES + OpQ::BYTES, S::WAVES * TURN / 2);
+    __shared__ __align__(1024) char lds0[STAGE];
+    __shared__ __align__(1024) char lds1[STAGE];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wp = wave & 3, wq = wave >> 2;
+    const int wp = wave % WP, wq = wave / WP;
     const TilePlace at = tile_place((a.np + TP - 1) / TP, (a.nq + TQ - 1) / TQ);
     const int64_t p0 = at.p * TP, q0 = at.q * TQ, piece = at.piece;
-    const int64_t cb = piece * a.piece, ce = min(a.nc, cb + a.piece);
+    const int cb = (int)(piece * a.piece), ce = (int)min(a.nc, (piece + 1) * a.piece);
 
     OpP P;
     OpQ Q;
@@ -227,7 +250,7 @@ __global__ __launch_bounds__(TTHREADS) void k_lin_tile(LinArgs a) {
     Q.place(a.Q, a.ldq, q0, a.nq, cb);
     // the sums begin with the bias: p = 32 i + 8 g + 4 (lane / 32) + e of
     // accumulator i's element 4 g + e
-    f32x16 acc[2][4];
+    f32x16 acc[2][FQ];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         f32x16 b = {};
@@ -241,52 +264,63 @@ __global__ __launch_bounds__(TTHREADS) void k_lin_tile(LinArgs a) {
                 for (int e = 0; e < 4; ++e) b[4 * g + e] = v[e];
             }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = b;
+        for (int j = 0; j < FQ; ++j) acc[i][j] = b;
     }
     // dbias: where it is asked for, the tiles of the first p sum Q's columns,
     // each wave those of one fragment
     const bool sums = OP == OP_DW && a.dbias && p0 == 0;
     float sum = 0.0f;
-    Reader<KQ, 1> RS;
-    RS.place(wq * 128 + wp * 32);
+    Reader<KQ, TQ, 1> RS;
+    RS.place(wq * (32 * FQ) + (wp < FQ ? wp : 0) * 32);
 
-    Reader<KP, 2> RP;
-    Reader<KQ, 4> RQ;
+    Reader<KP, TP, 2> RP;
+    Reader<KQ, TQ, FQ> RQ;
     RP.place(wp * 64);
-    RQ.place(wq * 128);
+    RQ.place(wq * (32 * FQ));
     const int64_t nb = (a.np + CK_COLS - 1) / CK_COLS, pb = min(p0 / CK_COLS + wp / 2, nb - 1);
 
-    // one stage: the next one's loads into `fill`, the products of `use`
-    const auto load = [&](char* fill, int64_t left) {
-        P.load(fill, left);
-        Q.load(fill + OpP::BYTES, left);
-    };
-    const auto stage = [&](char* __restrict fill, const char* __restrict use, int64_t c) {
+    // a stage's loads go out with its first two steps
+    constexpr auto first = [](int s, int loads) { return s < 2 ? s * loads / 2 : loads; };
+    // One stage: the products of `use`, and in their shade the next stage's
+    // loads into `fill` and each 16 c's fragments before they are needed.
+    const auto stage = [&](char* __restrict fill, const char* __restrict use, int c) {
         __builtin_amdgcn_s_waitcnt(WAIT_LOADS);
         __syncthreads();
-        if (c + TK < ce) load(fill, ce - c - TK);
+        const int left = ce - c - TK;
         int32_t word[2] = {0, 0};
         if constexpr (OP == OP_DW) {
             word[0] = cld(a.zexps, c / CK_ROWS * nb + pb);
-            word[1] = cld(a.zexps, min(c / CK_ROWS + 1, (a.nc - 1) / CK_ROWS) * nb + pb);
+            word[1] = cld(a.zexps, min(c / CK_ROWS + 1, (int)(a.nc - 1) / CK_ROWS) * nb + pb);
         }
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            F p[2], q[4];
+        F p[2][2], q[2][FQ];
+        const auto read = [&](int s) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 if constexpr (OP == OP_DW)
-                    p[i] = decode_fragment<T, E5>(RP.read_codes(use, i, s), word[s / 2]);
+                    p[s & 1][i] = decode_fragment<T, E5>(RP.read_codes(use, i, s), word[s / 2]);
                 else
-                    p[i] = RP.template read<T>(use, i, s);
+                    p[s & 1][i] = RP.template read<T>(use, i, s);
             }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) q[j] = RQ.template read<T>(use + OpP::BYTES, j, s);
+            for (int j = 0; j < FQ; ++j) q[s & 1][j] = RQ.template read<T>(use + OpP::BYTES, j, s);
+        };
+        read(0);
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+        for (int s = 0; s < 4; ++s) {
 #pragma unroll
-                for (int i = 0; i < 2; ++i) acc[i][j] = Mat<T>::mma(p[i], q[j], acc[i][j]);
+            for (int n = first(s, OpP::LOADS); n < first(s + 1, OpP::LOADS); ++n) P.load(fill, n, left);
+#pragma unroll
+            for (int n = first(s, OpQ::LOADS); n < first(s + 1, OpQ::LOADS); ++n) Q.load(fill + OpP::BYTES, n, left);
+            if (s < 3) read(s + 1);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int j = 0; j < FQ; ++j)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) acc[i][j] = Mat<T>::mma(p[s & 1][i], q[s & 1][j], acc[i][j]);
+            __builtin_amdgcn_sched_barrier(0);
         }
+        P.next();
+        Q.next();
         if (OP == OP_DW && sums) {
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
@@ -296,18 +330,26 @@ __global__ __launch_bounds__(TTHREADS) void k_lin_tile(LinArgs a) {
             }
         }
     };
-    if (cb < ce) load(lds0, ce - cb);
-    for (int64_t c = cb; c < ce; c += 2 * TK) {
+    if (cb < ce) {
+        const int left = ce - cb;
+#pragma unroll
+        for (int n = 0; n < OpP::LOADS; ++n) P.load(lds0, n, left);
+#pragma unroll
+        for (int n = 0; n < OpQ::LOADS; ++n) Q.load(lds0 + OpP::BYTES, n, left);
+        P.next();
+        Q.next();
+    }
+    for (int c = cb; c < ce; c += 2 * TK) {
         stage(lds1, lds0, c);
         if (c + TK < ce) stage(lds0, lds1, c + TK);
     }
 
     // accumulator [i][j]: q = its lane of 32, p = 4 elements of each 8, by the lane's half
-    const int64_t ql = q0 + wq * 128;
+    const int64_t ql = q0 + wq * (32 * FQ);
     if constexpr (OP == OP_DW) {
         sum += __shfl_xor(sum, 32);
         const int64_t q = ql + wp * 32 + lane;
-        if (sums && lane < 32 && q < a.nq) {
+        if (sums && wp < FQ && lane < 32 && q < a.nq) {
             if (a.split > 1)
                 a.part_bias[piece * a.nq + q] = sum;
             else
@@ -315,13 +357,13 @@ __global__ __launch_bounds__(TTHREADS) void k_lin_tile(LinArgs a) {
         }
     }
     __syncthreads();  // the stages are read out
-    int32_t word[4] = {0, 0, 0, 0};
+    int32_t word[FQ] = {};
     if constexpr (OP == OP_FWD) {
         if (a.codes) {
             // a block of 32 q x 128 p is two waves': its maximum goes by LDS
             uint32_t* red = (uint32_t*)lds0;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < FQ; ++j) {
                 float m = 0.0f, bad = 0.0f;
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
@@ -340,12 +382,12 @@ __global__ __launch_bounds__(TTHREADS) void k_lin_tile(LinArgs a) {
                             mx = ck_max_join(mx, ck_max_bits(ck_clamp(acc[i][j][e], ck_limit<T, E5>())));
                 }
                 mx = ck_wave_max(ql + j * 32 + (lane & 31) < a.nq ? mx : 0);
-                if (lane == 0) red[wave * 4 + j] = mx;
+                if (lane == 0) red[wave * FQ + j] = mx;
             }
             __syncthreads();
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                word[j] = ck_word(ck_max_join(red[wave * 4 + j], red[(wave ^ 1) * 4 + j]), ck_emax<E5>());
+            for (int j = 0; j < FQ; ++j) {
+                word[j] = ck_word(ck_max_join(red[wave * FQ + j], red[(wave ^ 1) * FQ + j]), ck_emax<E5>());
                 const int64_t qb = ql / CK_ROWS + j;
                 if ((wp & 1) == 0 && lane == 0 && qb * CK_ROWS < a.nq && p0 + wp * 64 < a.np)
                     a.exps[qb * nb + p0 / CK_COLS + wp / 2] = word[j];
@@ -353,35 +395,35 @@ __global__ __launch_bounds__(TTHREADS) void k_lin_tile(LinArgs a) {
             __syncthreads();
         }
     }
-    // Each wave turns its accumulators through 16 KB of LDS of its own, 64 q x
-    // 64 p at a time, so that eight lanes store a row's 64 p; a 16-byte chunk
-    // of row q lies at chunk ^ q & 15.
-    char* turn = (wave < 4 ? lds0 : lds1) + (wave & 3) * TURN_BYTES;
+    // Each wave turns its accumulators through LDS of its own, 32 RF q x 64 p
+    // at a time, so that eight lanes store a row's 64 p; a 16-byte chunk of row
+    // q lies at chunk ^ q & 15.
+    char* turn = (wave < S::WAVES / 2 ? lds0 : lds1) + wave % (S::WAVES / 2) * TURN;
     const int64_t p = p0 + wp * 64 + (lane & 7) * 8, have = a.np - p;
     with_act(OP == OP_DW || a.split > 1 ? APS_ACT_NONE : a.act, [&](auto act) {
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            const int64_t qr = ql + r * 64;
+        for (int r = 0; r < FQ / RF; ++r) {
+            const int64_t qr = ql + r * (32 * RF);
             if (qr >= a.nq) break;
-            LinRead<T, OP, 8> in[8];
+            LinRead<T, OP, 8> in[4 * RF];
             if (a.split == 1)
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
+                for (int k = 0; k < 4 * RF; ++k) {
                     const int64_t q = qr + k * 8 + (lane >> 3);
                     in[k].read(a, q, p, q < a.nq ? have : 0);
                 }
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+            for (int j = 0; j < RF; ++j)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const f32x16& v = acc[i / 4][2 * r + j];
+                    const f32x16& v = acc[i / 4][RF * r + j];
                     const int row = j * 32 + (lane & 31), chunk = (i / 4) * 8 + (i % 4) * 2 + (lane >> 5);
                     *(f32x4*)(turn + row * 256 + (chunk ^ (row & 15)) * 16) =
                         f32x4{v[i % 4 * 4], v[i % 4 * 4 + 1], v[i % 4 * 4 + 2], v[i % 4 * 4 + 3]};
                 }
             wave_lds_sync();
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
+            for (int k = 0; k < 4 * RF; ++k) {
                 const int row = k * 8 + (lane >> 3);
                 const int64_t q = qr + row;
                 const f32x4 lo = *(const f32x4*)(turn + row * 256 + (((lane & 7) * 2) ^ (row & 15)) * 16);
@@ -395,7 +437,7 @@ __global__ __launch_bounds__(TTHREADS) void k_lin_tile(LinArgs a) {
                     continue;
                 }
                 if (OP == OP_FWD && a.codes) {
-                    const int ft = ck_ft(word[2 * r + k / 4]);
+                    const int ft = ck_ft(word[RF * r + k / 4]);
                     lin_save4<T, E5>(a, q, p, have, ft, v);
                     lin_save4<T, E5>(a, q, p + 4, have - 4, ft, v + 4);
                 }
@@ -408,21 +450,55 @@ __global__ __launch_bounds__(TTHREADS) void k_lin_tile(LinArgs a) {
 
 }  // namespace
 
-int lin_tile_split(int64_t np, int64_t nq, int64_t nc) {
-    const int64_t tiles = ((np + TP - 1) / TP) * ((nq + TQ - 1) / TQ);
-    return (int)std::max<int64_t>(1, std::min<int64_t>(256 / tiles, nc / 256));
+// Pieces of the contraction, of at least 256 elements, where the tiles are
+// fewer than the workgroups that the GPU's 256 CUs hold at a time.
+LinTile lin_tile(int64_t np, int64_t nq, int64_t nc) {
+    const auto tiles = [&](int64_t tp, int64_t tq) { return ((np + tp - 1) / tp) * ((nq + tq - 1) / tq); };
+    LinTile t{0, 1};
+    const int64_t big = tiles(Big::TP, Big::TQ), middle = tiles(Middle::TP, Middle::TQ), small = tiles(Small::TP, Small::TQ);
+    const auto split = [&](int64_t n, int64_t fill) { return (int)std::max<int64_t>(1, std::min(fill / n, nc / 256)); };
+    t.shape = LIN_BIG;
+    t.split = split(big, 256);
+    if (big * t.split < 192) {
+        t.shape = LIN_MIDDLE;
+        t.split = split(middle, 512);
+        if (middle * t.split < 384) {
+            t.shape = LIN_SMALL;
+            t.split = split(small, 768);
+        }
+    }
+    return t;
 }
 
-void launch_lin_tile(int op, int dtype, bool e5, const LinArgs& a, hipStream_t s) {
-    const int64_t tiles = ((a.np + TP - 1) / TP) * ((a.nq + TQ - 1) / TQ);
-    const dim3 grid((unsigned)(tiles * a.split));
-#define APS_TILE(T) APS_LIN_OPS(k_lin_tile, T, grid, dim3(TTHREADS), 0, s, a)
-    if (dtype == APS_DTYPE_BF16) {
-        APS_TILE(__bf16)
-    } else {
-        APS_TILE(_Float16)
-    }
-#undef APS_TILE
+template <class T, int OP, bool E5>
+static void launch_shape(int shape, const LinArgs& a, hipStream_t s) {
+    const auto go = [&](auto sh) {
+        typedef decltype(sh) S;
+        const int64_t tiles = ((a.np + S::TP - 1) / S::TP) * ((a.nq + S::TQ - 1) / S::TQ);
+        hipLaunchKernelGGL((k_lin_tile<T, OP, E5, S>), dim3((unsigned)(tiles * a.split)), dim3(S::THREADS), 0, s, a);
+    };
+    if (shape == LIN_BIG)
+        go(Big());
+    else if (shape == LIN_MIDDLE)
+        go(Middle());
+    else
+        go(Small());
+}
+
+void launch_lin_tile(int op, int dtype, bool e5, int shape, const LinArgs& a, hipStream_t s) {
+    const auto with = [&](auto t) {
+        typedef decltype(t) T;
+        if (op == OP_FWD)
+            e5 ? launch_shape<T, OP_FWD, true>(shape, a, s) : launch_shape<T, OP_FWD, false>(shape, a, s);
+        else if (op == OP_DX)
+            e5 ? launch_shape<T, OP_DX, true>(shape, a, s) : launch_shape<T, OP_DX, false>(shape, a, s);
+        else
+            e5 ? launch_shape<T, OP_DW, true>(shape, a, s) : launch_shape<T, OP_DW, false>(shape, a, s);
+    };
+    if (dtype == APS_DTYPE_BF16)
+        with((__bf16)0.0f);
+    else
+        with((_Float16)0.0f);
 }
 
 }  // namespace aps
