@@ -511,7 +511,19 @@ def _dtype_codes():
 
 def _matrix(t, name: str, dtypes, dev=None, shape=None) -> int:
     """The row stride of a 2-D GPU tensor of one of ``dtypes`` with unit column
-    stride, on ``dev`` and of ``shape``."""
+    stride, on ``dev`` and of ``shape``.  One pass over the properties where all
+    is well (0.4 us); what is wrong is found out afterwards."""
+    try:
+        rows, cols = t.shape
+        ld, step = t.stride()
+        if (t.is_cuda and t.dtype in dtypes and (dev is None or t.device == dev)
+                and (shape is None or (rows, cols) == shape) and (step == 1 or cols <= 1)):
+            if rows <= 1 or cols == 0:  # an empty or one-row tensor may report any row stride
+                return cols or 1
+            if ld >= cols:
+                return ld
+    except (AttributeError, TypeError, ValueError):
+        pass
     if not getattr(t, "is_cuda", False):
         raise ValueError(f"{name} must be a GPU tensor" + ("" if t is None else f", got {type(t).__name__}"))
     if t.dim() != 2:
@@ -520,16 +532,9 @@ def _matrix(t, name: str, dtypes, dev=None, shape=None) -> int:
         raise ValueError(f"{name} must be of dtype {' or '.join(str(d) for d in dtypes)}, got {t.dtype}")
     if dev is not None and t.device != dev:
         raise ValueError(f"{name} is on {t.device}, the other arrays on {dev}")
-    rows, cols = t.shape
-    if shape is not None and (rows, cols) != shape:
+    if shape is not None and tuple(t.shape) != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
-    if rows <= 1 or cols == 0:  # an empty or one-row tensor may report any row stride
-        if cols > 1 and t.stride(1) != 1:
-            raise ValueError(f"{name} needs unit column stride")
-        return max(cols, 1)
-    if (cols > 1 and t.stride(1) != 1) or t.stride(0) < cols:
-        raise ValueError(f"{name} needs unit column stride and rows that do not overlap")
-    return t.stride(0)
+    raise ValueError(f"{name} needs unit column stride and rows that do not overlap")
 
 
 def _ckpt_words(M: int, C: int) -> tuple:
@@ -546,12 +551,11 @@ def _ckpt(codes, ckpt_exp, dev, shape) -> int:
     return ldc
 
 
-def _new_ckpt(M: int, C: int, codes, ckpt_exp, dev):
-    import torch
+def _new_ckpt(M: int, C: int, codes, ckpt_exp, like, stream):
     if codes is None:
-        codes = torch.empty((M, C), dtype=torch.uint8, device=dev)
+        codes = _fresh(like, (M, C), stream, _dtypes(*_U8)[0])
     if ckpt_exp is None:
-        ckpt_exp = torch.empty(_ckpt_words(M, C), dtype=torch.int32, device=dev)
+        ckpt_exp = _fresh(like, _ckpt_words(M, C), stream, _dtypes(*_I32)[0])
     return codes, ckpt_exp
 
 
@@ -561,23 +565,39 @@ def aps_linear_workspace_bytes(op: int, M: int, N: int, K: int, dtype) -> int:
     return int(lib().aps_linear_workspace_bytes(int(op), int(M), int(N), int(K), _dtype_codes()[dtype]))
 
 
-def _linear_workspace(op: int, M: int, N: int, K: int, dtype: int, workspace, dev):
+def _fresh(like, size, stream, dtype=None):
+    """A new array beside ``like``.  Where the call goes to a stream of its own,
+    the memory is that stream's: what is freed after the call is used again
+    in its order only."""
+    if stream is None:
+        return like.new_empty(size, dtype=dtype)
+    import torch
+    with torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream):
+        return like.new_empty(size, dtype=dtype)
+
+
+@functools.lru_cache(maxsize=4096)
+def _linear_need(op: int, M: int, N: int, K: int, dtype: int) -> int:
+    return int(lib().aps_linear_workspace_bytes(op, M, N, K, dtype))
+
+
+def _linear_workspace(op: int, M: int, N: int, K: int, dtype: int, workspace, like, stream):
     """(tensor, bytes) of the call's workspace; allocated where it is missing and needed."""
     if workspace is None:
-        import torch
-        need = int(lib().aps_linear_workspace_bytes(op, M, N, K, dtype))
+        need = _linear_need(op, M, N, K, dtype)
         if need == 0:
             return None, 0
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-    _need(workspace, "workspace", _dtypes(*_U8), 0, dev)
+        return _fresh(like, need, stream, _dtypes(*_U8)[0]), need
+    _need(workspace, "workspace", _dtypes(*_U8), 0, like.device)
     return workspace, workspace.numel()
 
 
 def _float_input(t, name: str) -> tuple:
     """(row stride, the one-element tuple of its dtype, its APS_DTYPE) of an
     activation or gradient."""
-    ld = _matrix(t, name, tuple(_dtype_codes()))
-    return ld, (t.dtype,), _dtype_codes()[t.dtype]
+    codes = _dtype_codes()
+    ld = _matrix(t, name, codes)
+    return ld, (t.dtype,), codes[t.dtype]
 
 
 def aps_linear(X, W, bias=None, residual=None, act: int = APS_ACT_NONE, Y=None, ckpt_fmt: Format | None = None,
@@ -585,7 +605,6 @@ def aps_linear(X, W, bias=None, residual=None, act: int = APS_ACT_NONE, Y=None, 
     """Y = act(X W^T + bias) + residual for W [out features][in features].
     With ``ckpt_fmt`` the pre-activation X W^T + bias is also kept in 8 bits.
     Missing outputs are allocated here.  Returns Y, or (Y, codes, ckpt_exp)."""
-    import torch
     ldx, T, dt = _float_input(X, "X")
     dev = X.device
     M, K = X.shape
@@ -597,15 +616,15 @@ def aps_linear(X, W, bias=None, residual=None, act: int = APS_ACT_NONE, Y=None, 
         _need(bias, "bias", T, N, dev)
     ldr = 0 if residual is None else _matrix(residual, "residual", T, dev, (M, N))
     if Y is None:
-        Y = torch.empty((M, N), dtype=X.dtype, device=dev)
+        Y = _fresh(X, (M, N), stream)
     ldy = _matrix(Y, "Y", T, dev, (M, N))
     ldc = 0
     if ckpt_fmt is not None:
-        codes, ckpt_exp = _new_ckpt(M, N, codes, ckpt_exp, dev)
+        codes, ckpt_exp = _new_ckpt(M, N, codes, ckpt_exp, X, stream)
         ldc = _ckpt(codes, ckpt_exp, dev, (M, N))
     elif codes is not None or ckpt_exp is not None:
         raise ValueError("codes and ckpt_exp need ckpt_fmt")
-    ws, nbytes = _linear_workspace(APS_LINEAR_FORWARD, M, N, K, dt, workspace, dev)
+    ws, nbytes = _linear_workspace(APS_LINEAR_FORWARD, M, N, K, dt, workspace, X, stream)
     _check("aps_linear", lib().aps_linear(
         _ptr(X), ldx, _ptr(W), ldw, _ptr(bias), _ptr(residual), ldr, _ptr(Y), ldy, M, N, K, dt, int(act),
         _NO_FORMAT if ckpt_fmt is None else ckpt_fmt.c(), _ptr(codes), ldc, _ptr(ckpt_exp), _ptr(ws), nbytes,
@@ -617,7 +636,6 @@ def aps_linear_grad_input(dZ, W, residual=None, act: int = APS_ACT_NONE, codes=N
                           fmt: Format | None = None, dX=None, workspace=None, stream=None):
     """dX = (dZ W) * act'(z) + residual, z being the checkpointed
     pre-activation that made this layer's input (none with APS_ACT_NONE)."""
-    import torch
     ldz, T, dt = _float_input(dZ, "dZ")
     dev = dZ.device
     M, N = dZ.shape
@@ -627,7 +645,7 @@ def aps_linear_grad_input(dZ, W, residual=None, act: int = APS_ACT_NONE, codes=N
         raise ValueError(f"inner dimensions differ: dZ has {N} columns, W {W.shape[0]} rows")
     ldr = 0 if residual is None else _matrix(residual, "residual", T, dev, (M, K))
     if dX is None:
-        dX = torch.empty((M, K), dtype=dZ.dtype, device=dev)
+        dX = _fresh(dZ, (M, K), stream)
     ldx = _matrix(dX, "dX", T, dev, (M, K))
     ldc = 0
     if int(act) != APS_ACT_NONE:
@@ -636,7 +654,7 @@ def aps_linear_grad_input(dZ, W, residual=None, act: int = APS_ACT_NONE, codes=N
         ldc = _ckpt(codes, ckpt_exp, dev, (M, K))
     elif codes is not None or ckpt_exp is not None or fmt is not None:
         raise ValueError("a checkpoint is read for an activation's derivative only: act is none")
-    ws, nbytes = _linear_workspace(APS_LINEAR_GRAD_INPUT, M, N, K, dt, workspace, dev)
+    ws, nbytes = _linear_workspace(APS_LINEAR_GRAD_INPUT, M, N, K, dt, workspace, dZ, stream)
     _check("aps_linear_grad_input", lib().aps_linear_grad_input(
         _ptr(dZ), ldz, _ptr(W), ldw, _ptr(residual), ldr, int(act), _NO_FORMAT if fmt is None else fmt.c(),
         _ptr(codes), ldc, _ptr(ckpt_exp), _ptr(dX), ldx, M, N, K, dt, _ptr(ws), nbytes, _stream(stream, dev)))
@@ -648,7 +666,6 @@ def aps_linear_grad_weight(dZ, codes, ckpt_exp, fmt: Format, dW=None, dbias=None
     """dW = dZ^T X in fp32, X from its checkpoint; with a ``dbias`` tensor also
     the column sums of dZ.  ``accumulate`` adds to dW and dbias.  dW may be a
     view of a row of G: ``G[w, o:o + N * K].view(N, K)``."""
-    import torch
     ldz, _, dt = _float_input(dZ, "dZ")
     dev = dZ.device
     M, N = dZ.shape
@@ -659,10 +676,10 @@ def aps_linear_grad_weight(dZ, codes, ckpt_exp, fmt: Format, dW=None, dbias=None
     if dW is None:
         if accumulate:
             raise ValueError("accumulate needs dW")
-        dW = torch.empty((N, K), dtype=torch.float32, device=dev)
+        dW = _fresh(dZ, (N, K), stream, _dtypes(*_F32)[0])
     lddw = _matrix(dW, "dW", _dtypes(*_F32), dev, (N, K))
     _need(dbias, "dbias", _dtypes(*_F32), N, dev, optional=True)
-    ws, nbytes = _linear_workspace(APS_LINEAR_GRAD_WEIGHT, M, N, K, dt, workspace, dev)
+    ws, nbytes = _linear_workspace(APS_LINEAR_GRAD_WEIGHT, M, N, K, dt, workspace, dZ, stream)
     _check("aps_linear_grad_weight", lib().aps_linear_grad_weight(
         _ptr(dZ), ldz, fmt.c(), _ptr(codes), ldc, _ptr(ckpt_exp), _ptr(dW), lddw, _ptr(dbias), M, N, K, dt,
         APS_GRAD_ACCUMULATE if accumulate else 0, _ptr(ws), nbytes, _stream(stream, dev)))
@@ -671,13 +688,12 @@ def aps_linear_grad_weight(dZ, codes, ckpt_exp, fmt: Format, dW=None, dbias=None
 
 def aps_activation_grad(dY, codes, ckpt_exp, fmt: Format, act: int, dZ=None, stream=None):
     """dZ = dY * act'(z), z from its checkpoint; dZ may be dY."""
-    import torch
     ldy, T, dt = _float_input(dY, "dY")
     dev = dY.device
     M, C = dY.shape
     ldc = _ckpt(codes, ckpt_exp, dev, (M, C))
     if dZ is None:
-        dZ = torch.empty((M, C), dtype=dY.dtype, device=dev)
+        dZ = _fresh(dY, (M, C), stream)
     ldz = _matrix(dZ, "dZ", T, dev, (M, C))
     _check("aps_activation_grad", lib().aps_activation_grad(
         _ptr(dY), ldy, int(act), fmt.c(), _ptr(codes), ldc, _ptr(ckpt_exp), _ptr(dZ), ldz, M, C, dt,
@@ -690,7 +706,7 @@ def aps_checkpoint_save(X, fmt: Format, codes=None, ckpt_exp=None, stream=None):
     ldx, _, dt = _float_input(X, "X")
     dev = X.device
     M, C = X.shape
-    codes, ckpt_exp = _new_ckpt(M, C, codes, ckpt_exp, dev)
+    codes, ckpt_exp = _new_ckpt(M, C, codes, ckpt_exp, X, stream)
     ldc = _ckpt(codes, ckpt_exp, dev, (M, C))
     _check("aps_checkpoint_save", lib().aps_checkpoint_save(_ptr(X), ldx, M, C, dt, fmt.c(), _ptr(codes), ldc,
                                                             _ptr(ckpt_exp), _stream(stream, dev)))
@@ -699,17 +715,16 @@ def aps_checkpoint_save(X, fmt: Format, codes=None, ckpt_exp=None, stream=None):
 
 def aps_checkpoint_load(codes, ckpt_exp, fmt: Format, act: int = APS_ACT_NONE, X=None, dtype=None, stream=None):
     """act(the checkpoint's values), into X or a new tensor of ``dtype``."""
-    import torch
     ldc = _ckpt(codes, ckpt_exp, None, None)
     dev = codes.device
     M, C = codes.shape
     if X is None:
         if dtype not in _dtype_codes():
             raise ValueError(f"dtype must be float32, bfloat16 or float16, got {dtype}")
-        X = torch.empty((M, C), dtype=dtype, device=dev)
+        X = _fresh(codes, (M, C), stream, dtype)
     elif dtype is not None and X.dtype != dtype:
         raise ValueError(f"X is of dtype {X.dtype}, not {dtype}")
-    ldx = _matrix(X, "X", tuple(_dtype_codes()), dev, (M, C))
+    ldx = _matrix(X, "X", _dtype_codes(), dev, (M, C))
     _check("aps_checkpoint_load", lib().aps_checkpoint_load(_ptr(codes), ldc, _ptr(ckpt_exp), M, C, fmt.c(), int(act),
                                                             _ptr(X), ldx, _dtype_codes()[X.dtype],
                                                             _stream(stream, dev)))

@@ -20,15 +20,17 @@ Dims dims_of(int op, int64_t M, int64_t N, int64_t K) {
 
 int64_t part_stride(int64_t np) { return (np + 3) / 4 * 4; }
 
-enum Kernel { GENERAL, TILE };
+enum Kernel { GENERAL, TILE, DECODE };
 struct Plan {
     Kernel kernel;
     int shape, split;
 };
 
-// `fast`: the operands' rows are aligned for the tile kernel.
-Plan plan_of(int op, const Dims& d, int dtype, bool fast) {
+// `fast`: the operands' rows are aligned for the tile kernel; `plain`: no
+// checkpoint is written.
+Plan plan_of(int op, const Dims& d, int dtype, bool fast, bool plain) {
     if (d.np == 0 || d.nq == 0) return {GENERAL, 0, 1};
+    if (op == OP_FWD && plain && d.nq <= LIN_FEW) return {DECODE, 0, 1};
     if (fast && dtype != APS_DTYPE_F32) {
         const LinTile t = lin_tile(d.np, d.nq, d.nc);
         return {TILE, t.shape, t.split};
@@ -37,16 +39,16 @@ Plan plan_of(int op, const Dims& d, int dtype, bool fast) {
 }
 
 uint64_t workspace_of(int op, const Dims& d, int dtype) {
-    const int64_t s = std::max(plan_of(op, d, dtype, false).split, plan_of(op, d, dtype, true).split);
+    const int64_t s = std::max(plan_of(op, d, dtype, false, false).split, plan_of(op, d, dtype, true, false).split);
     return s > 1 ? (uint64_t)(s * d.nq * (part_stride(d.np) + (op == OP_DW ? 1 : 0))) * 4 : 0;
 }
 
 int launch_product(int op, int dtype, bool e5, LinArgs& a, void* workspace, hipStream_t s) {
     // rows of whole 16-byte chunks, and offsets within a tile that fit 31 bits
-    const int pe = op == OP_DW ? 16 : 8;
-    const bool fast = aligned16(a.P) && aligned16(a.Q) && a.ldp % pe == 0 && a.ldq % 8 == 0 && a.ldp < (1 << 22) &&
-                      a.ldq < (1 << 22) && (op == OP_FWD ? a.nc : a.np) % pe == 0 && (op == OP_DW ? a.nq : a.nc) % 8 == 0;
-    const Plan plan = plan_of(op, {a.np, a.nq, a.nc}, dtype, fast);
+    const int e = 16 / lin_elem_bytes(dtype), pe = op == OP_DW ? 16 : e;
+    const bool fast = aligned16(a.P) && aligned16(a.Q) && a.ldp % pe == 0 && a.ldq % e == 0 && a.ldp < (1 << 22) &&
+                      a.ldq < (1 << 22) && (op == OP_FWD ? a.nc : a.np) % pe == 0 && (op == OP_DW ? a.nq : a.nc) % e == 0;
+    const Plan plan = plan_of(op, {a.np, a.nq, a.nc}, dtype, fast, !a.codes);
     a.split = plan.split;
     a.piece = ((a.nc + a.split - 1) / a.split + 63) / 64 * 64;
     if (a.split > 1) {
@@ -54,7 +56,9 @@ int launch_product(int op, int dtype, bool e5, LinArgs& a, void* workspace, hipS
         a.part = (float*)workspace;
         a.part_bias = a.part + a.split * a.nq * a.ldpart;
     }
-    if (plan.kernel == TILE)
+    if (plan.kernel == DECODE)
+        launch_lin_decode(dtype, fast, a, s);
+    else if (plan.kernel == TILE)
         launch_lin_tile(op, dtype, e5, plan.shape, a, s);
     else
         launch_lin_general(op, dtype, e5, a, s);

@@ -438,6 +438,9 @@ int lin_split(int op, int64_t np, int64_t nq, int64_t nc, int dtype);
 void launch_lin_general(int op, int dtype, bool e5, const LinArgs& a, hipStream_t s);
 void launch_lin_join(int op, int dtype, bool e5, const LinArgs& a, hipStream_t s);
 
+constexpr int LIN_FEW = 32;  // rows that the decode kernel takes
+void launch_lin_decode(int dtype, bool fast, const LinArgs& a, hipStream_t s);
+
 // The tile kernel's shapes, and its choice for an output and a contraction.
 enum LinShape : int32_t { LIN_BIG, LIN_MIDDLE, LIN_SMALL };
 struct LinTile {

@@ -202,61 +202,61 @@ __global__ __launch_bounds__(GTHREADS) void k_lin_general(LinArgs a) {
 }
 
 // The sum of a split contraction's pieces, in their order, and the epilogue:
-// a workgroup finishes one checkpoint block of 32 q x 128 p.
+// a workgroup finishes one checkpoint block of 32 q x 128 p, a thread four p.
+constexpr int JTHREADS = 1024;
+
 template <class T, int OP, bool E5>
-__global__ __launch_bounds__(GTHREADS) void k_lin_join(LinArgs a) {
-    __shared__ uint32_t red[GTHREADS / 64];
+__global__ __launch_bounds__(JTHREADS) void k_lin_join(LinArgs a) {
+    __shared__ uint32_t red[JTHREADS / 64];
     const int64_t tp = (a.np + CK_COLS - 1) / CK_COLS;
     const int64_t pb = blockIdx.x % tp, qb = blockIdx.x / tp;
-    const int64_t p = pb * CK_COLS + threadIdx.x % 32 * 4, have = a.np - p;
-    const int64_t q0 = qb * CK_ROWS + threadIdx.x / 32;
-    float v[4][4] = {};
-    float b[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (OP == OP_FWD) lin_bias4<T>(a, p, have, b);
-    uint32_t mx = 0;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int64_t q = q0 + 8 * j;
-        if (q >= a.nq || have <= 0) continue;
-        const float* in = a.part + q * a.ldpart + p;
-        for (int s = 0; s < a.split; ++s) {
-            const f32x4 x = *(const f32x4*)(in + s * a.nq * a.ldpart);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[j][e] += x[e];
+    const int64_t p = pb * CK_COLS + threadIdx.x % 32 * 4, q = qb * CK_ROWS + threadIdx.x / 32;
+    const int64_t have = q < a.nq ? a.np - p : 0;
+    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+    LinRead<T, OP, 4> in;
+    in.read(a, q, p, have);
+    if (have > 0) {
+        const int64_t step = a.nq * a.ldpart;
+        const float* x = a.part + q * a.ldpart + p;
+        int s = 0;
+        for (; s + 4 <= a.split; s += 4, x += 4 * step) {  // four pieces in flight
+            const f32x4 x0 = *(const f32x4*)x, x1 = *(const f32x4*)(x + step), x2 = *(const f32x4*)(x + 2 * step),
+                        x3 = *(const f32x4*)(x + 3 * step);
+            v = (((v + x0) + x1) + x2) + x3;
         }
+        for (; s < a.split; ++s, x += step) v += *(const f32x4*)x;
+    }
+    if (OP == OP_FWD) {
+        float b[4];
+        lin_bias4<T>(a, p, have, b);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            v[j][e] += b[e];
-            if (OP == OP_FWD && a.codes && e < have)
-                mx = ck_max_join(mx, ck_max_bits(ck_clamp(v[j][e], ck_limit<T, E5>())));
-        }
+        for (int e = 0; e < 4; ++e) v[e] += b[e];
     }
     if (OP == OP_DW && a.dbias && pb == 0 && threadIdx.x < 32 && qb * CK_ROWS + threadIdx.x < a.nq) {
-        const int64_t q = qb * CK_ROWS + threadIdx.x;
+        const int64_t r = qb * CK_ROWS + threadIdx.x;
         float db = 0.0f;
-        for (int s = 0; s < a.split; ++s) db += a.part_bias[s * a.nq + q];
-        a.dbias[q] = a.accumulate ? a.dbias[q] + db : db;
+        for (int s = 0; s < a.split; ++s) db += a.part_bias[s * a.nq + r];
+        a.dbias[r] = a.accumulate ? a.dbias[r] + db : db;
     }
     int32_t word = 0;
     if (OP == OP_FWD && a.codes) {
+        uint32_t mx = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < have) mx = ck_max_join(mx, ck_max_bits(ck_clamp(v[e], ck_limit<T, E5>())));
         mx = ck_wave_max(mx);
         if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = mx;
         __syncthreads();
-        word = ck_word(ck_max_join(ck_max_join(red[0], red[1]), ck_max_join(red[2], red[3])), ck_emax<E5>());
+#pragma unroll
+        for (int w = 0; w < JTHREADS / 64; ++w) mx = ck_max_join(mx, red[w]);
+        word = ck_word(mx, ck_emax<E5>());
         if (threadIdx.x == 0) a.exps[qb * tp + pb] = word;
     }
     if (have <= 0) return;
-    with_act(OP == OP_DW ? APS_ACT_NONE : a.act, [&](auto act) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int64_t q = q0 + 8 * j;
-            if (q >= a.nq) break;
-            if (OP == OP_FWD && a.codes) lin_save4<T, E5>(a, q, p, have, ck_ft(word), v[j]);
-            LinRead<T, OP, 4> in;
-            in.read(a, q, p, have);
-            lin_finish<T, OP, E5, 4, act.value>(a, in, q, p, have, v[j]);
-        }
-    });
+    const float z[4] = {v[0], v[1], v[2], v[3]};
+    if (OP == OP_FWD && a.codes) lin_save4<T, E5>(a, q, p, have, ck_ft(word), z);
+    with_act(OP == OP_DW ? APS_ACT_NONE : a.act,
+             [&](auto act) { lin_finish<T, OP, E5, 4, act.value>(a, in, q, p, have, z); });
 }
 
 }  // namespace
@@ -286,7 +286,7 @@ void launch_lin_general(int op, int dtype, bool e5, const LinArgs& a, hipStream_
 
 void launch_lin_join(int op, int dtype, bool e5, const LinArgs& a, hipStream_t s) {
     const dim3 grid((unsigned)(((a.np + CK_COLS - 1) / CK_COLS) * ((a.nq + CK_ROWS - 1) / CK_ROWS)));
-    APS_LIN_TYPES(k_lin_join, grid, dim3(GTHREADS), 0, s, a)
+    APS_LIN_TYPES(k_lin_join, grid, dim3(JTHREADS), 0, s, a)
 }
 
 }  // namespace aps
