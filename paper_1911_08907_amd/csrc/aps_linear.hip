@@ -31,8 +31,8 @@ struct Plan {
 Plan plan_of(int op, const Dims& d, int dtype, bool fast, bool plain) {
     if (d.np == 0 || d.nq == 0) return {GENERAL, 0, 1};
     if (op == OP_FWD && plain && d.nq <= LIN_FEW) return {DECODE, 0, 1};
-    if (fast && dtype != APS_DTYPE_F32) {
-        const LinTile t = lin_tile(d.np, d.nq, d.nc);
+    if (fast) {
+        const LinTile t = lin_tile(op, d.np, d.nq, d.nc, dtype == APS_DTYPE_F32);
         return {TILE, t.shape, t.split};
     }
     return {GENERAL, 0, lin_split(op, d.np, d.nq, d.nc, dtype)};

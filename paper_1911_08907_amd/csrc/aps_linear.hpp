@@ -446,7 +446,7 @@ enum LinShape : int32_t { LIN_BIG, LIN_MIDDLE, LIN_SMALL };
 struct LinTile {
     int shape, split;
 };
-LinTile lin_tile(int64_t np, int64_t nq, int64_t nc);
+LinTile lin_tile(int op, int64_t np, int64_t nq, int64_t nc, bool f32);
 void launch_lin_tile(int op, int dtype, bool e5, int shape, const LinArgs& a, hipStream_t s);
 
 }  // namespace aps

@@ -1,25 +1,28 @@
-// aps_linear_tile.hip -- the linear layer's products of 16-bit operands whose
-// rows are aligned to 16 bytes.
+// aps_linear_tile.hip -- the linear layer's products of operands whose rows
+// are aligned to 16 bytes.
 //
 // A workgroup forms a tile of 256 p x 256 q with eight waves (two on each
 // SIMD), 128 x 128 with four, or 128 x 64 with four; each wave two by four, two
-// or one 32 x 32 accumulators.  The contraction is staged 64 deep in two
-// buffers of LDS that the loads fill directly.  A stage's loads are issued
+// or one 32 x 32 accumulators.  The contraction is staged 128 bytes
+// deep (64 c of a 16-bit type, 32 of fp32) in two buffers of LDS that the loads fill directly.  A stage's loads are issued
 // in the first half of the stage before, so one barrier per stage suffices: it
 // says both that the stage has landed and that the other buffer is read out.
-// Within a stage a fragment is read one step of 16 c before its products.
+// Within a stage a fragment is read one of four steps before its products.
 //
 // In LDS a stage lies as it does in memory, each 16-byte chunk of a row at a
 // place exclusive-ored with a few bits of the row, which the loading lane
 // chooses by the chunk it asks for:
-//   along rows   [rows][64 c]: a fragment is one 16-byte read per lane;
+//   along rows   [rows][128 bytes]: a fragment is one 16-byte read per lane;
 //                chunk ^ (row / 2) & 7 gives 16 lanes 64 different banks
-//   row to row   [64 c][p]: a fragment is two transposing reads of 4 c x 16 p
-//                per 16 lanes; chunk ^ 4 (c & 3) gives 32 lanes all banks
-//   codes        [64 c][p] bytes: one transposing read of 8 c x 16 p per 16
+//   row to row   [c][p]: a fragment is two transposing reads of 4 c x 16 p per
+//                16 lanes; chunk ^ 4 (c & 3) gives 32 lanes all banks.  fp32: four
+//                reads of one c x 32 p; chunk ^ 8 (c / 8 & 1) parts the halves
+//   codes        [c][p] bytes: one transposing read of 8 c x 16 p per 16
 //                lanes, chunk ^ 2 (c & 7) (rows of 256; half of that for 128);
 //                then four conversions of two codes, with the block's power of
 //                two, to the matrix type: exact
+// An fp32 step is 8 c by four instructions of 2: a lane's half h holds 4 c from
+// 16 (s / 2) + 8 h + 4 (s & 1) on in step s, so that two steps are one read of codes.
 // Elements past an operand's end are read as zero by the buffer loads' own
 // range check, through an offset that is out of range.
 #include "aps_linear.hpp"
@@ -28,7 +31,8 @@ namespace aps {
 
 namespace {
 
-constexpr int TK = 64;  // contraction elements of a stage
+template <class T>
+constexpr int TK_OF = 128 / (int)sizeof(T);  // contraction elements of a stage
 
 // FQ accumulators of 32 q by two of 32 p a wave, WP x WQ waves.
 template <int FQ_, int WP_, int WQ_>
@@ -85,6 +89,17 @@ struct Mat<_Float16> {
     }
 };
 
+template <>
+struct Mat<float> {
+    typedef f32x4 frag;
+    static __device__ __forceinline__ f32x16 mma(frag p, frag q, f32x16 c) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(p[i], q[i], c, 0, 0, 0);
+        return c;
+    }
+    static __device__ __forceinline__ float add2(uint32_t w, float s) { return s + u2f(w); }
+};
+
 enum Kind { ALONG, ACROSS, CODES };
 
 // What the place of a row-to-row operand's chunk is exclusive-ored with, in
@@ -93,14 +108,15 @@ enum Kind { ALONG, ACROSS, CODES };
 template <int R, int ELEM>
 __device__ __forceinline__ int across_xor(int c) {
     constexpr int PER = 256 / (R * ELEM) > 1 ? 256 / (R * ELEM) : 1;  // rows of 256 bytes
+    if constexpr (ELEM == 4) return (c / 8 & 1) * 8;
     if constexpr (ELEM == 1) return (c / PER & (8 / PER - 1)) * 2;
     return (c / PER & (4 / PER - 1)) * 4;
 }
 
 // One operand's R rows (p or q): what a lane loads.
-template <Kind KIND, int R, int WAVES>
+template <class T, Kind KIND, int R, int WAVES>
 struct Operand {
-    static constexpr int ELEM = KIND == CODES ? 1 : 2;
+    static constexpr int ELEM = KIND == CODES ? 1 : sizeof(T), TK = TK_OF<T>;
     static constexpr int BYTES = R * TK * ELEM;  // of a stage
     static constexpr int LOADS = BYTES / (WAVES * 1024);
     static_assert(LOADS * WAVES * 1024 == BYTES, "whole loads of every wave");
@@ -116,7 +132,7 @@ struct Operand {
             base = (const char*)p + (r0 * ld + c0) * ELEM;
             step = TK * ELEM;
             const int chunk = (lane & 7) ^ ((4 * wave + (lane >> 4)) & 7);
-            c_of = chunk * 8;
+            c_of = chunk * (16 / ELEM);
             c_step = 0;
 #pragma unroll
             for (int n = 0; n < LOADS; ++n) {
@@ -126,22 +142,22 @@ struct Operand {
         } else {
             constexpr int PER_ROW = R * ELEM / 16;        // chunks of a row
             constexpr int ROWS = 64 / PER_ROW;            // rows of one load
-            static_assert(WAVES * ROWS % 8 == 0, "the exclusive-or is the same for each of a lane's loads");
             base = (const char*)p + (c0 * ld + r0) * ELEM;
             step = TK * ld * ELEM;
             const int c = ROWS * wave + lane / PER_ROW;
-            const int chunk = (lane % PER_ROW) ^ across_xor<R, ELEM>(c);
             c_of = c;
             c_step = WAVES * ROWS;
 #pragma unroll
-            for (int n = 0; n < LOADS; ++n)
+            for (int n = 0; n < LOADS; ++n) {
+                const int chunk = (lane % PER_ROW) ^ across_xor<R, ELEM>(c + n * c_step);
                 off[n] = r0 + chunk * (16 / ELEM) < nr
                              ? (uint32_t)(c + n * c_step) * (uint32_t)(ld * ELEM) + chunk * 16
                              : OUT_OF_RANGE;
+            }
         }
     }
-    // The n-th load of a stage with `left` c's (at least 64 but at the end of
-    // the contraction, none or fewer after it) into LDS.
+    // The n-th load of a stage into LDS; `left` c's are left, none or fewer
+    // behind the contraction's end.
     __device__ __forceinline__ void load(char* lds, int n, int left) const {
         const __amdgpu_buffer_rsrc_t rsrc =
             __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)OUT_OF_RANGE, 0x00020000);
@@ -156,7 +172,7 @@ struct Operand {
 // differ from fragment to fragment and from 16 c to 16 c by constants, but for
 // the exclusive-or: along rows it depends on the 16 c, otherwise on the
 // fragment's rows.
-template <Kind KIND, int R, int N>
+template <class T, Kind KIND, int R, int N>
 struct Reader {
     static constexpr int BASES = KIND == ALONG ? 4 : N;
     int at[BASES];
@@ -166,7 +182,11 @@ struct Reader {
         for (int b = 0; b < BASES; ++b) {
             if constexpr (KIND == ALONG) {
                 const int row = lane & 31;
-                at[b] = (r + row) * 128 + ((2 * b + half) ^ ((row >> 1) & 7)) * 16;
+                const int chunk = sizeof(T) == 4 ? b / 2 * 4 + half * 2 + b % 2 : 2 * b + half;
+                at[b] = (r + row) * 128 + (chunk ^ ((row >> 1) & 7)) * 16;
+            } else if constexpr (KIND == ACROSS && sizeof(T) == 4) {
+                const int c = half * 8, p = r + 32 * b + (lane & 31);
+                at[b] = c * (4 * R) + ((p >> 2) ^ across_xor<R, 4>(c)) * 16 + (p & 3) * 4;
             } else if constexpr (KIND == ACROSS) {
                 const int c = half * 8 + (i >> 2), p = r + 32 * b + (lane & 16) + (i & 3) * 4;
                 at[b] = c * (2 * R) + ((p >> 3) ^ across_xor<R, 2>(c)) * 16 + (p & 7) * 2;
@@ -176,26 +196,41 @@ struct Reader {
             }
         }
     }
-    // fragment n of the s-th 16 c
-    template <class T>
+    // fragment n of step s
     __device__ __forceinline__ typename Mat<T>::frag read(const char* lds, int n, int s) const {
         typedef typename Mat<T>::frag F;
         if constexpr (KIND == ALONG) return *(const F*)(lds + at[s] + n * 32 * 128);
+        if constexpr (sizeof(T) == 4) {
+            const char* p = lds + at[KIND == ALONG ? 0 : n] + (s / 2 * 16 + s % 2 * 4) * (4 * R);
+            F v;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = *(const float*)(p + i * (4 * R));
+            return v;
+        }
         const char* p = lds + at[KIND == ALONG ? 0 : n] + s * 16 * (2 * R);
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(APS_LDS(s16x4, p));
         const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(APS_LDS(s16x4, p + 4 * (2 * R)));
         struct { s16x4 a, b; } both = {lo, hi};
         return __builtin_bit_cast(F, both);
     }
+    // fragment n's codes of the s-th 16 c
     __device__ __forceinline__ i32x2 read_codes(const char* lds, int n, int s) const {
         return __builtin_amdgcn_ds_read_tr8_b64_v2i32(APS_LDS(i32x2, lds + at[n] + s * 16 * R));
     }
 };
 
 template <class T, bool E5>
-__device__ __forceinline__ typename Mat<T>::frag decode_fragment(i32x2 w, int32_t word) {
+__device__ __forceinline__ typename Mat<T>::frag decode_fragment(i32x2 w, int32_t word, int s) {
     typedef Mat<T> M;
     const float inv = pow2_of(-ck_ft(word));
+    if constexpr (sizeof(T) == 4) {
+        f32x4 d;
+        float z[4];
+        ck_decode4<E5>((uint32_t)w[s % 2], inv, word & CK_ODD, z);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) d[i] = z[i];
+        return d;
+    } else {
     u4v v = {M::template two<E5, false>(w[0], inv), M::template two<E5, true>(w[0], inv),
              M::template two<E5, false>(w[1], inv), M::template two<E5, true>(w[1], inv)};
     if (!E5 && (word & CK_ODD)) {  // the conversion knows no INF of 1-4-3
@@ -207,6 +242,7 @@ __device__ __forceinline__ typename Mat<T>::frag decode_fragment(i32x2 w, int32_
         }
     }
     return __builtin_bit_cast(typename M::frag, v);
+    }
 }
 
 // Which tile and piece a workgroup forms.  Workgroups go to the eight XCDs in
@@ -226,11 +262,11 @@ __device__ __forceinline__ TilePlace tile_place(int64_t tp, int64_t tq) {
 
 template <class T, int OP, bool E5, class S>
 __global__ __launch_bounds__(S::THREADS, 2) void k_lin_tile(LinArgs a) {
-    constexpr int FQ = S::FQ, WP = S::WP, TP = S::TP, TQ = S::TQ;
+    constexpr int FQ = S::FQ, WP = S::WP, TP = S::TP, TQ = S::TQ, TK = TK_OF<T>;
     constexpr Kind KP = OP == OP_FWD ? ALONG : (OP == OP_DX ? ACROSS : CODES);
     constexpr Kind KQ = OP == OP_DW ? ACROSS : ALONG;
-    typedef Operand<KP, TP, S::WAVES> OpP;
-    typedef Operand<KQ, TQ, S::WAVES> OpQ;
+    typedef Operand<T, KP, TP, S::WAVES> OpP;
+    typedef Operand<T, KQ, TQ, S::WAVES> OpQ;
     typedef typename Mat<T>::frag F;
     // the epilogue turns a wave's accumulators through LDS, RF of its FQ at a time
     constexpr int RF = FQ < 2 ? FQ : 2, TURN = RF * 32 * 64 * 4;
@@ -270,11 +306,11 @@ __global__ __launch_bounds__(S::THREADS, 2) void k_lin_tile(LinArgs a) {
     // each wave those of one fragment
     const bool sums = OP == OP_DW && a.dbias && p0 == 0;
     float sum = 0.0f;
-    Reader<KQ, TQ, 1> RS;
+    Reader<T, KQ, TQ, 1> RS;
     RS.place(wq * (32 * FQ) + (wp < FQ ? wp : 0) * 32);
 
-    Reader<KP, TP, 2> RP;
-    Reader<KQ, TQ, FQ> RQ;
+    Reader<T, KP, TP, 2> RP;
+    Reader<T, KQ, TQ, FQ> RQ;
     RP.place(wp * 64);
     RQ.place(wq * (32 * FQ));
     const int64_t nb = (a.np + CK_COLS - 1) / CK_COLS, pb = min(p0 / CK_COLS + wp / 2, nb - 1);
@@ -293,16 +329,21 @@ __global__ __launch_bounds__(S::THREADS, 2) void k_lin_tile(LinArgs a) {
             word[1] = cld(a.zexps, min(c / CK_ROWS + 1, (int)(a.nc - 1) / CK_ROWS) * nb + pb);
         }
         F p[2][2], q[2][FQ];
+        i32x2 codes[2];
         const auto read = [&](int s) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 if constexpr (OP == OP_DW)
-                    p[s & 1][i] = decode_fragment<T, E5>(RP.read_codes(use, i, s), word[s / 2]);
+                    {
+                    const int g = sizeof(T) == 4 ? s / 2 : s;  // fp32: two steps from one read
+                    if (g == s || s % 2 == 0) codes[i] = RP.read_codes(use, i, g);
+                    p[s & 1][i] = decode_fragment<T, E5>(codes[i], word[sizeof(T) == 4 ? 0 : s / 2], s);
+                }
                 else
-                    p[s & 1][i] = RP.template read<T>(use, i, s);
+                    p[s & 1][i] = RP.read(use, i, s);
             }
 #pragma unroll
-            for (int j = 0; j < FQ; ++j) q[s & 1][j] = RQ.template read<T>(use + OpP::BYTES, j, s);
+            for (int j = 0; j < FQ; ++j) q[s & 1][j] = RQ.read(use + OpP::BYTES, j, s);
         };
         read(0);
 #pragma unroll
@@ -324,7 +365,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void k_lin_tile(LinArgs a) {
         if (OP == OP_DW && sums) {
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
-                const u4v w = __builtin_bit_cast(u4v, RS.template read<T>(use + OpP::BYTES, 0, s));
+                const u4v w = __builtin_bit_cast(u4v, RS.read(use + OpP::BYTES, 0, s));
 #pragma unroll
                 for (int i = 0; i < 4; ++i) sum = Mat<T>::add2(w[i], sum);
             }
@@ -450,24 +491,43 @@ __global__ __launch_bounds__(S::THREADS, 2) void k_lin_tile(LinArgs a) {
 
 }  // namespace
 
-// Pieces of the contraction, of at least 256 elements, where the tiles are
-// fewer than the workgroups that the GPU's 256 CUs hold at a time.
-LinTile lin_tile(int64_t np, int64_t nq, int64_t nc) {
-    const auto tiles = [&](int64_t tp, int64_t tq) { return ((np + tp - 1) / tp) * ((nq + tq - 1) / tq); };
-    LinTile t{0, 1};
-    const int64_t big = tiles(Big::TP, Big::TQ), middle = tiles(Middle::TP, Middle::TQ), small = tiles(Small::TP, Small::TQ);
-    const auto split = [&](int64_t n, int64_t fill) { return (int)std::max<int64_t>(1, std::min(fill / n, nc / 256)); };
-    t.shape = LIN_BIG;
-    t.split = split(big, 256);
-    if (big * t.split < 192) {
-        t.shape = LIN_MIDDLE;
-        t.split = split(middle, 512);
-        if (middle * t.split < 384) {
-            t.shape = LIN_SMALL;
-            t.split = split(small, 768);
+// The shape and the pieces of the contraction that a model of the time finds
+// fastest, in us: a launch; per stage the latency of one tile's stage or,
+// where more tiles are at work, their share of the GPU; per tile its epilogue;
+// for a split the join's launch and the partial sums' way out and in.  The
+// terms were fitted to graph replays of 40 products from 64 x 64 x 16384 to
+// 16384 x 4096 x 1024, where the model's choice took at most 1.16 times the best
+// of all shapes with 1 to 32 pieces (in us: 512 x 4096 x 1024 bf16, small 9.8, middle
+// 12.1, big 27.8; 4096 x 4096 x 1024, small 50.5, middle 43.5, big 36.5; 64 x
+// 1024 x 4096, small in 8 pieces 10.4, in 2 17.7).
+LinTile lin_tile(int op, int64_t np, int64_t nq, int64_t nc, bool f32) {
+    static const struct {
+        int shape, tp, tq, fill;       // tiles at work at a time
+        double launch, stage, decode;  // once; a stage alone; one that decodes
+        double share, tile;            // a stage per tile; a tile
+    } half[] = {{LIN_BIG, 256, 256, 256, 6.5, 1.3, 1.5, 0.0063, 0.02},
+                {LIN_MIDDLE, 128, 128, 512, 4.5, 0.42, 1.0, 0.0020, 0.008},
+                {LIN_SMALL, 128, 64, 768, 3.2, 0.35, 0.8, 0.00125, 0.004}},
+      full[] = {{LIN_MIDDLE, 128, 128, 512, 4.5, 2.0, 2.2, 0.0077, 0.008},
+                {LIN_MIDDLE, 128, 128, 512, 4.5, 2.0, 2.2, 0.0077, 0.008},
+                {LIN_SMALL, 128, 64, 768, 3.2, 1.1, 1.3, 0.0039, 0.004}};
+    LinTile best{LIN_SMALL, 1};
+    double least = 1e300;
+    const int64_t stages = (nc + (f32 ? 31 : 63)) / (f32 ? 32 : 64);
+    for (const auto& m : f32 ? full : half) {
+        const int64_t tiles = ((np + m.tp - 1) / m.tp) * ((nq + m.tq - 1) / m.tq);
+        for (int64_t split = 1; split <= 64 && split * 4 <= std::max<int64_t>(stages, 4); split += split < 4 ? 1 : split / 2) {
+            const double n = (double)(tiles * split);
+            if (split > 1 && n > 2 * m.fill) break;
+            const double turns = std::ceil(n / m.fill);  // a last turn that is not full takes half a full one's time
+            const double work = std::max(n, (turns - 1) * m.fill + std::min(n, 0.5 * m.fill));
+            double t = m.launch + std::ceil((double)stages / split) * std::max(op == OP_DW ? m.decode : m.stage, m.share * work) +
+                       m.tile * n;
+            if (split > 1) t += 4.0 + (double)split * np * nq * 8 / 6.0e6;
+            if (t < least) least = t, best = {m.shape, (int)split};
         }
     }
-    return t;
+    return best;
 }
 
 template <class T, int OP, bool E5>
@@ -477,9 +537,9 @@ static void launch_shape(int shape, const LinArgs& a, hipStream_t s) {
         const int64_t tiles = ((a.np + S::TP - 1) / S::TP) * ((a.nq + S::TQ - 1) / S::TQ);
         hipLaunchKernelGGL((k_lin_tile<T, OP, E5, S>), dim3((unsigned)(tiles * a.split)), dim3(S::THREADS), 0, s, a);
     };
-    if (shape == LIN_BIG)
-        go(Big());
-    else if (shape == LIN_MIDDLE)
+    if constexpr (sizeof(T) == 2)
+        if (shape == LIN_BIG) return go(Big());
+    if (shape == LIN_MIDDLE)
         go(Middle());
     else
         go(Small());
@@ -497,8 +557,10 @@ void launch_lin_tile(int op, int dtype, bool e5, int shape, const LinArgs& a, hi
     };
     if (dtype == APS_DTYPE_BF16)
         with((__bf16)0.0f);
-    else
+    else if (dtype == APS_DTYPE_F16)
         with((_Float16)0.0f);
+    else
+        with(0.0f);
 }
 
 }  // namespace aps
