@@ -20,8 +20,8 @@
  * stride in elements, at least the row's length; pointers are aligned to
  * their element.  Rows aligned to 16 bytes (pointer and stride) and lengths
  * that are multiples of 8 run fastest; no alignment or length is refused.
- * Sizes: M, N, K in [0, 2^22] with every matrix at most 2^23 blocks of
- * 32 x 128 (2^35 elements); row strides up to 2^31 - 1.  Arrays that a
+ * Sizes: M, N, K in [0, 2^22] with every matrix at most 2^22 blocks of
+ * 32 x 128 (2^34 elements); row strides up to 2^31 - 1.  Arrays that a
  * call does not touch (a dimension is 0) may be NULL.
  *
  * Checkpoints.  A matrix [M][C] is kept as one code byte per element,

@@ -144,12 +144,15 @@ __global__ __launch_bounds__(CTHREADS) void k_ckpt_save(CkArgs a) {
             float v[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] = (float)x[s][4 * g + i];
-            if (careful)
+            if (careful) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = ck_clamp(v[i], lim);
+                for (int i = 0; i < 4; ++i) v[i] = ck_clamp(v[i], lim) * up;
+                c[g] = ck_encode4<E5>(v);
+            } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] *= up;
-            c[g] = ck_encode4<E5>(v);
+                for (int i = 0; i < 4; ++i) v[i] *= up;
+                c[g] = ck_encode4_finite<E5>(v);
+            }
         }
         uint8_t* o = a.codes + r * a.ldc + w.col;
         if (VEC && w.have >= E) {

@@ -24,31 +24,70 @@ enum Kernel { GENERAL, TILE, DECODE };
 struct Plan {
     Kernel kernel;
     int shape, split;
+    bool copy_p, copy_q;  // operands that the tile kernel reads from aligned copies
 };
 
-// `fast`: the operands' rows are aligned for the tile kernel; `plain`: no
-// checkpoint is written.
-Plan plan_of(int op, const Dims& d, int dtype, bool fast, bool plain) {
-    if (d.np == 0 || d.nq == 0) return {GENERAL, 0, 1};
-    if (op == OP_FWD && plain && d.nq <= LIN_FEW) return {DECODE, 0, 1};
-    if (fast) {
-        const LinTile t = lin_tile(op, d.np, d.nq, d.nc, dtype == APS_DTYPE_F32);
-        return {TILE, t.shape, t.split};
+// Elements of an operand's 16-byte chunk, and whether its rows are whole ones.
+int chunk_p(int op, int dtype) { return op == OP_DW ? 16 : 16 / lin_elem_bytes(dtype); }
+int chunk_q(int dtype) { return 16 / lin_elem_bytes(dtype); }
+int64_t row_p(int op, const Dims& d) { return op == OP_FWD ? d.nc : d.np; }
+int64_t row_q(int op, const Dims& d) { return op == OP_DW ? d.nq : d.nc; }
+int64_t rows_p(int op, const Dims& d) { return op == OP_FWD ? d.np : d.nc; }
+int64_t rows_q(int op, const Dims& d) { return op == OP_DW ? d.nc : d.nq; }
+
+int64_t whole(int64_t n, int64_t chunk) { return (n + chunk - 1) / chunk * chunk; }
+uint64_t copy_bytes(int64_t rows, int64_t row, int chunk) { return (uint64_t)(rows * whole(row, chunk)) * (16 / chunk) + 256; }
+
+// `aligned`: operands whose rows are whole chunks also start on them.  `plain`:
+// no checkpoint is written.  An operand whose rows are no whole chunks is
+// copied where the model says so: in us, a launch and its bytes in and out.
+Plan plan_of(int op, const Dims& d, int dtype, bool aligned, bool plain) {
+    if (d.np == 0 || d.nq == 0) return {GENERAL, 0, 1, false, false};
+    if (op == OP_FWD && plain && d.nq <= LIN_FEW) return {DECODE, 0, 1, false, false};
+    const bool f32 = dtype == APS_DTYPE_F32;
+    const int cp = chunk_p(op, dtype), cq = chunk_q(dtype);
+    const bool copy_p = row_p(op, d) % cp != 0, copy_q = row_q(op, d) % cq != 0;
+    const LinTile g = lin_general(op, d.np, d.nq, d.nc, f32);
+    // a stage's offsets within a tile fit 31 bits, a copy's threads a launch
+    const int64_t most = (int64_t)1 << 32;
+    if (aligned && row_p(op, d) < (1 << 21) && row_q(op, d) < (1 << 21) && !(copy_p && rows_p(op, d) * row_p(op, d) > most) &&
+        !(copy_q && rows_q(op, d) * row_q(op, d) > most)) {
+        const LinTile t = lin_tile(op, d.np, d.nq, d.nc, f32);
+        double us = t.us;
+        if (copy_p || copy_q) us += 3.0;
+        if (copy_p) us += (double)copy_bytes(rows_p(op, d), row_p(op, d), cp) / 1.5e6;
+        if (copy_q) us += (double)copy_bytes(rows_q(op, d), row_q(op, d), cq) / 1.5e6;
+        if (!(copy_p || copy_q) || us < g.us) return {TILE, t.shape, t.split, copy_p, copy_q};
     }
-    return {GENERAL, 0, lin_split(op, d.np, d.nq, d.nc, dtype)};
+    return {GENERAL, 0, g.split, false, false};
+}
+
+// Partial sums, then the copies.
+uint64_t part_bytes(int op, const Dims& d, int split) {
+    return split > 1 ? ((uint64_t)(split * d.nq * (part_stride(d.np) + (op == OP_DW ? 1 : 0))) * 4 + 255) / 256 * 256 : 0;
 }
 
 uint64_t workspace_of(int op, const Dims& d, int dtype) {
-    const int64_t s = std::max(plan_of(op, d, dtype, false, false).split, plan_of(op, d, dtype, true, false).split);
-    return s > 1 ? (uint64_t)(s * d.nq * (part_stride(d.np) + (op == OP_DW ? 1 : 0))) * 4 : 0;
+    uint64_t most = 0;
+    for (int aligned = 0; aligned < 2; ++aligned) {
+        const Plan p = plan_of(op, d, dtype, aligned, false);
+        uint64_t n = part_bytes(op, d, p.split);
+        if (p.copy_p) n += copy_bytes(rows_p(op, d), row_p(op, d), chunk_p(op, dtype));
+        if (p.copy_q) n += copy_bytes(rows_q(op, d), row_q(op, d), chunk_q(dtype));
+        most = std::max(most, n);
+    }
+    return most;
 }
 
+// A pointer and stride on whole chunks, for an operand that is read in place.
+bool on_chunks(const void* p, int64_t ld, int chunk) { return aligned16(p) && ld % chunk == 0 && ld < (1 << 21); }
+
 int launch_product(int op, int dtype, bool e5, LinArgs& a, void* workspace, hipStream_t s) {
-    // rows of whole 16-byte chunks, and offsets within a tile that fit 31 bits
-    const int e = 16 / lin_elem_bytes(dtype), pe = op == OP_DW ? 16 : e;
-    const bool fast = aligned16(a.P) && aligned16(a.Q) && a.ldp % pe == 0 && a.ldq % e == 0 && a.ldp < (1 << 22) &&
-                      a.ldq < (1 << 22) && (op == OP_FWD ? a.nc : a.np) % pe == 0 && (op == OP_DW ? a.nq : a.nc) % e == 0;
-    const Plan plan = plan_of(op, {a.np, a.nq, a.nc}, dtype, fast, !a.codes);
+    const Dims d{a.np, a.nq, a.nc};
+    const int cp = chunk_p(op, dtype), cq = chunk_q(dtype);
+    const bool in_place_p = on_chunks(a.P, a.ldp, cp), in_place_q = on_chunks(a.Q, a.ldq, cq);
+    const bool aligned = (in_place_p || row_p(op, d) % cp != 0) && (in_place_q || row_q(op, d) % cq != 0);
+    const Plan plan = plan_of(op, d, dtype, aligned, !a.codes);
     a.split = plan.split;
     a.piece = ((a.nc + a.split - 1) / a.split + 63) / 64 * 64;
     if (a.split > 1) {
@@ -56,8 +95,22 @@ int launch_product(int op, int dtype, bool e5, LinArgs& a, void* workspace, hipS
         a.part = (float*)workspace;
         a.part_bias = a.part + a.split * a.nq * a.ldpart;
     }
+    if (plan.copy_p || plan.copy_q) {
+        char* to = (char*)workspace + part_bytes(op, d, a.split);
+        LinCopy p{}, q{};
+        if (plan.copy_p) {
+            p = {a.P, to, a.ldp, whole(row_p(op, d), cp), rows_p(op, d), row_p(op, d), 16 / cp};
+            to += (copy_bytes(p.rows, p.cols, cp) + 15) / 16 * 16;
+            a.P = p.dst, a.ldp = p.ldd;
+        }
+        if (plan.copy_q) {
+            q = {a.Q, to, a.ldq, whole(row_q(op, d), cq), rows_q(op, d), row_q(op, d), 16 / cq};
+            a.Q = q.dst, a.ldq = q.ldd;
+        }
+        launch_lin_align(p, q, s);
+    }
     if (plan.kernel == DECODE)
-        launch_lin_decode(dtype, fast, a, s);
+        launch_lin_decode(dtype, in_place_p && in_place_q && a.nc % cq == 0, a, s);
     else if (plan.kernel == TILE)
         launch_lin_tile(op, dtype, e5, plan.shape, a, s);
     else

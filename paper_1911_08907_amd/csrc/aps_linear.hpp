@@ -212,6 +212,14 @@ __device__ __forceinline__ uint32_t ck_encode4(const float v[4]) {
     return encode4_e4m3(v[0], v[1], v[2], v[3]);
 }
 
+// The same for finite values within the format's largest magnitude.
+template <bool E5>
+__device__ __forceinline__ uint32_t ck_encode4_finite(const float v[4]) {
+    if constexpr (E5)
+        return (uint32_t)__builtin_amdgcn_cvt_pk_bf8_f32(v[2], v[3], __builtin_amdgcn_cvt_pk_bf8_f32(v[0], v[1], 0, false), true);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], 0, false), true);
+}
+
 // 1-4-3's INF and NaN among four codes: v where a code is one.
 __device__ __forceinline__ void ck_odd_e4m3(uint32_t w, float v[4]) {
 #pragma unroll
@@ -368,21 +376,29 @@ __device__ __forceinline__ void lin_bias4(const LinArgs& a, int64_t p, int64_t h
         b[0] = b[1] = b[2] = b[3] = 0.0f;
 }
 
-// The codes of four values of z at row q, with the block's exponent known.
+// The codes of four values of z at row q, with the block's word known.
 template <class T, bool E5>
-__device__ __forceinline__ void lin_save4(const LinArgs& a, int64_t q, int64_t p, int64_t have, int ft, const float z[4]) {
+__device__ __forceinline__ void lin_save4(const LinArgs& a, int64_t q, int64_t p, int64_t have, int32_t word, const float z[4]) {
     constexpr float lim = ck_limit<T, E5>();
-    const float s = pow2_of(ft);
+    const float s = pow2_of(ck_ft(word));
     float v[4];
+    uint32_t c;
+    if (word & CK_ODD) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = ck_clamp(z[i], lim) * s;
-    store_some_codes(a.codes + q * a.ldcodes + p, have, a.vec & LV_CODES, ck_encode4<E5>(v));
+        for (int i = 0; i < 4; ++i) v[i] = ck_clamp(z[i], lim) * s;
+        c = ck_encode4<E5>(v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = __builtin_amdgcn_fmed3f(z[i], -lim, lim) * s;
+        c = ck_encode4_finite<E5>(v);
+    }
+    store_some_codes(a.codes + q * a.ldcodes + p, have, a.vec & LV_CODES, c);
 }
 
 // ------------------------------------------------------------ host checks
 
 constexpr int64_t LIN_MAX_LD = (1LL << 31) - 1;
-constexpr int64_t LIN_MAX_BLOCKS = 1 << 23;  // blocks of 32 x 128: a launch's size stays within HIP's
+constexpr int64_t LIN_MAX_BLOCKS = 1 << 22;  // blocks of 32 x 128: a launch's size stays within HIP's
 
 static inline int lin_elem_bytes(int dtype) { return dtype == APS_DTYPE_F32 ? 4 : 2; }
 
@@ -434,19 +450,30 @@ static inline int lin_check_checkpoint(aps_format f, const void* codes, int64_t 
 // ------------------------------------------------------------ the launches
 
 // dtype is one of APS_DTYPE_*; the format is 1-5-2 (e5) or 1-4-3.
-int lin_split(int op, int64_t np, int64_t nq, int64_t nc, int dtype);
 void launch_lin_general(int op, int dtype, bool e5, const LinArgs& a, hipStream_t s);
 void launch_lin_join(int op, int dtype, bool e5, const LinArgs& a, hipStream_t s);
 
 constexpr int LIN_FEW = 32;  // rows that the decode kernel takes
 void launch_lin_decode(int dtype, bool fast, const LinArgs& a, hipStream_t s);
 
-// The tile kernel's shapes, and its choice for an output and a contraction.
+// One operand's copy into aligned rows (src NULL: none).
+struct LinCopy {
+    const void* src;
+    void* dst;
+    int64_t lds, ldd, rows, cols;  // row strides in elements; ldd is whole 16-byte chunks
+    int32_t elem;                  // bytes
+};
+void launch_lin_align(const LinCopy& p, const LinCopy& q, hipStream_t s);
+
+// A choice for an output and a contraction: the tile kernel's shape, the pieces
+// of the contraction, and the model's time in us.
 enum LinShape : int32_t { LIN_BIG, LIN_MIDDLE, LIN_SMALL };
 struct LinTile {
     int shape, split;
+    double us;
 };
 LinTile lin_tile(int op, int64_t np, int64_t nq, int64_t nc, bool f32);
+LinTile lin_general(int op, int64_t np, int64_t nq, int64_t nc, bool f32);
 void launch_lin_tile(int op, int dtype, bool e5, int shape, const LinArgs& a, hipStream_t s);
 
 }  // namespace aps

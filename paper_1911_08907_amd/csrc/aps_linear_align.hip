@@ -1,0 +1,43 @@
+// aps_linear_align.hip -- copies of a product's operands whose rows are no
+// whole 16-byte chunks, into rows that are, filled up with zeros: a read and a
+// write of the operand, after which the tile kernel applies.
+#include "aps_linear.hpp"
+
+namespace aps {
+
+namespace {
+
+// A thread writes one chunk of 16 bytes.
+template <class W>
+__device__ __forceinline__ void align_chunk(const LinCopy& c, int64_t k) {
+    constexpr int E = 16 / (int)sizeof(W);
+    typedef W vec __attribute__((ext_vector_type(E)));
+    const int64_t per = c.ldd / E, r = k / per, col = k % per * E;
+    const W* s = (const W*)c.src + r * c.lds + col;
+    vec v = {};
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+        if (col + i < c.cols) v[i] = s[i];
+    *(vec*)((W*)c.dst + r * c.ldd + col) = v;
+}
+
+__global__ __launch_bounds__(256) void k_lin_align(LinCopy p, LinCopy q, int64_t np, int64_t nq) {
+    int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const bool second = k >= np;
+    const LinCopy& c = second ? q : p;
+    if (second) k -= np;
+    if (second && k >= nq) return;
+    if (c.elem == 1) align_chunk<uint8_t>(c, k);
+    else if (c.elem == 2) align_chunk<uint16_t>(c, k);
+    else align_chunk<uint32_t>(c, k);
+}
+
+}  // namespace
+
+void launch_lin_align(const LinCopy& p, const LinCopy& q, hipStream_t s) {
+    const auto chunks = [](const LinCopy& c) { return c.src ? c.rows * (c.ldd * c.elem / 16) : 0; };
+    const int64_t np = chunks(p), nq = chunks(q);
+    hipLaunchKernelGGL(k_lin_align, dim3((unsigned)((np + nq + 255) / 256)), dim3(256), 0, s, p, q, np, nq);
+}
+
+}  // namespace aps

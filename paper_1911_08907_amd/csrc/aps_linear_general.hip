@@ -182,7 +182,7 @@ __global__ __launch_bounds__(GTHREADS) void k_lin_general(LinArgs a) {
                 for (int i = 0; i < 8; ++i) {
                     const float z[4] = {acc[i / 4][i % 4 * 4], acc[i / 4][i % 4 * 4 + 1], acc[i / 4][i % 4 * 4 + 2],
                                         acc[i / 4][i % 4 * 4 + 3]};
-                    lin_save4<T, E5>(a, q, pl + 8 * i, a.np - pl - 8 * i, ck_ft(word), z);
+                    lin_save4<T, E5>(a, q, pl + 8 * i, a.np - pl - 8 * i, word, z);
                 }
         }
     }
@@ -254,7 +254,7 @@ __global__ __launch_bounds__(JTHREADS) void k_lin_join(LinArgs a) {
     }
     if (have <= 0) return;
     const float z[4] = {v[0], v[1], v[2], v[3]};
-    if (OP == OP_FWD && a.codes) lin_save4<T, E5>(a, q, p, have, ck_ft(word), z);
+    if (OP == OP_FWD && a.codes) lin_save4<T, E5>(a, q, p, have, word, z);
     with_act(OP == OP_DW ? APS_ACT_NONE : a.act,
              [&](auto act) { lin_finish<T, OP, E5, 4, act.value>(a, in, q, p, have, z); });
 }
@@ -263,10 +263,15 @@ __global__ __launch_bounds__(JTHREADS) void k_lin_join(LinArgs a) {
 
 // Pieces of the contraction: where the tiles are fewer than two workgroups
 // per CU, enough pieces for that many, of at least 128 contraction elements.
-int lin_split(int op, int64_t np, int64_t nq, int64_t nc, int dtype) {
+// The time in us as measured: a stage of 64 bytes takes 1.7 of latency (2.8
+// where it decodes), or 0.003 for each tile at work.
+LinTile lin_general(int op, int64_t np, int64_t nq, int64_t nc, bool f32) {
     const int64_t tiles = ((np + GP - 1) / GP) * ((nq + GQ - 1) / GQ);
-    if (tiles == 0) return 1;
-    return (int)std::max<int64_t>(1, std::min<int64_t>(512 / tiles, nc / 128));
+    const int64_t split = std::max<int64_t>(1, std::min<int64_t>(512 / std::max<int64_t>(tiles, 1), nc / 128));
+    const int64_t stages = (nc + (f32 ? 15 : 31)) / (f32 ? 16 : 32);
+    const double us = 3.0 + std::ceil((double)stages / split) * std::max(op == OP_DW ? 2.8 : 1.7, 0.003 * tiles * split) +
+                      (split > 1 ? 4.0 + (double)split * np * nq * 8 / 6.0e6 : 0.0);
+    return {LIN_SMALL, (int)split, us};
 }
 
 #define APS_LIN_TYPES(K, ...)                                              \

@@ -478,9 +478,9 @@ __global__ __launch_bounds__(S::THREADS, 2) void k_lin_tile(LinArgs a) {
                     continue;
                 }
                 if (OP == OP_FWD && a.codes) {
-                    const int ft = ck_ft(word[RF * r + k / 4]);
-                    lin_save4<T, E5>(a, q, p, have, ft, v);
-                    lin_save4<T, E5>(a, q, p + 4, have - 4, ft, v + 4);
+                    const int32_t wd = word[RF * r + k / 4];
+                    lin_save4<T, E5>(a, q, p, have, wd, v);
+                    lin_save4<T, E5>(a, q, p + 4, have - 4, wd, v + 4);
                 }
                 lin_finish<T, OP, E5, 8, act.value>(a, in[k], q, p, have, v);
             }
@@ -511,8 +511,7 @@ LinTile lin_tile(int op, int64_t np, int64_t nq, int64_t nc, bool f32) {
       full[] = {{LIN_MIDDLE, 128, 128, 512, 4.5, 2.0, 2.2, 0.0077, 0.008},
                 {LIN_MIDDLE, 128, 128, 512, 4.5, 2.0, 2.2, 0.0077, 0.008},
                 {LIN_SMALL, 128, 64, 768, 3.2, 1.1, 1.3, 0.0039, 0.004}};
-    LinTile best{LIN_SMALL, 1};
-    double least = 1e300;
+    LinTile best{LIN_SMALL, 1, 1e300};
     const int64_t stages = (nc + (f32 ? 31 : 63)) / (f32 ? 32 : 64);
     for (const auto& m : f32 ? full : half) {
         const int64_t tiles = ((np + m.tp - 1) / m.tp) * ((nq + m.tq - 1) / m.tq);
@@ -524,7 +523,7 @@ LinTile lin_tile(int op, int64_t np, int64_t nq, int64_t nc, bool f32) {
             double t = m.launch + std::ceil((double)stages / split) * std::max(op == OP_DW ? m.decode : m.stage, m.share * work) +
                        m.tile * n;
             if (split > 1) t += 4.0 + (double)split * np * nq * 8 / 6.0e6;
-            if (t < least) least = t, best = {m.shape, (int)split};
+            if (t < best.us) best = {m.shape, (int)split, t};
         }
     }
     return best;
