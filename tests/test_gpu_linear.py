@@ -584,3 +584,91 @@ def test_streams_and_workspaces(dev):
     with pytest.raises(A.ApsError) as e:
         A.aps_linear(X, W, b, r, workspace=torch.empty(need - 1, dtype=torch.uint8, device=dev))
     assert e.value.status == A.APS_ERR_SIZE
+
+
+# Products for every shape of the tile kernel (256 x 256, 128 x 128 and 128 x 64
+# tiles), split and whole, the few rows of a decoding step, and odd rows that
+# are copied; in float64 on the GPU.
+LARGE = [(700, 700, 700), (333, 1000, 520), (2304, 2048, 320), (4096, 4096, 128), (40, 4096, 512), (1, 4096, 1024),
+         (32, 1000, 4100), (20, 333, 77), (512, 520, 4096), (4096, 264, 520), (130, 2000, 1000)]
+
+
+@pytest.mark.parametrize("M,N,K", LARGE)
+@pytest.mark.parametrize("t", list(TYPES))
+def test_larger_products(dev, t, M, N, K):
+    T = TYPES[t]
+    g = torch.Generator(device=dev)
+    g.manual_seed(M + N + K)
+    rnd = lambda *s: torch.randn(*s, generator=g, device=dev)  # noqa: E731
+    X, W = rnd(M, K).to(T), (rnd(N, K) / math.sqrt(K)).to(T)
+    b, r, dZ = rnd(N).to(T), rnd(M, N).to(T), (rnd(M, N) / 16).to(T)
+    X64, W64, b64, r64, dZ64 = (v.double() for v in (X, W, b, r, dZ))
+    fmt = "1-4-3" if (M + N) % 2 else "1-5-2"
+    # forward, with and without a checkpoint
+    z = X64 @ W64.t() + b64
+    ez = R.sums_bound(W64.abs().t(), X64.abs(), b64.abs())
+    ref = R.act(z, "gelu") + r64
+    e = R.LIPSCHITZ * ez + R.ACT_ULPS * z.abs() + 2.0 ** -24 * ref.abs()
+    tol = e + R.half_step(T) * (ref.abs() + e) + R.tiny(T)
+    Y = A.aps_linear(X, W, b, r, ACT["gelu"])
+    assert bool(((Y.double() - ref).abs() <= tol).all())
+    Y, codes, words = A.aps_linear(X, W, b, r, ACT["gelu"], ckpt_fmt=FMT[fmt])
+    assert bool(((Y.double() - ref).abs() <= tol).all())
+    _check_zhat(codes, words, fmt, T, z.cpu(), ez.cpu())
+    # the input gradient at this checkpoint's shape: the layer below has N out features
+    s = R.slope(R.load(codes, words, fmt), "silu")
+    up = (rnd(M, K) / 16).to(T)          # the gradient of a layer with K out and N in features
+    W2 = (rnd(K, N) / math.sqrt(K)).to(T)
+    d = up.double() @ W2.double()
+    ref = d * s + r64
+    ed = R.sums_bound(W2.double().abs(), up.double().abs())
+    e = R.LIPSCHITZ * ed + d.abs() * 2 * R.ACT_ULPS + 2.0 ** -23 * ref.abs()
+    tol = e + R.half_step(T) * (ref.abs() + e) + R.tiny(T)
+    dX = A.aps_linear_grad_input(up, W2, r, ACT["silu"], codes, words, FMT[fmt])
+    assert bool(((dX.double() - ref).abs() <= tol).all())
+    # the weight gradient
+    cx, wx = A.aps_checkpoint_save(X, FMT[fmt])
+    x = R.load(cx, wx, fmt)
+    db = torch.empty(N, device=dev)
+    dW = A.aps_linear_grad_weight(dZ, cx, wx, FMT[fmt], dbias=db)
+    ref = dZ64.t() @ x
+    tol = R.sums_bound(x.abs(), dZ64.abs().t()) + 2.0 ** -24 * ref.abs()
+    assert bool(((dW.double() - ref).abs() <= tol).all())
+    assert bool(((db.double() - dZ64.sum(0)).abs() <= (M + 2) * 2.0 ** -23 * dZ64.abs().sum(0)).all())
+
+
+@pytest.mark.parametrize("t", ["bf16", "fp16"])
+def test_subnormal_operands_count(dev, t):
+    """The matrix instructions take the type's subnormals as they are."""
+    T = TYPES[t]
+    tiny = torch.finfo(T).smallest_normal
+    X = torch.full((40, 64), tiny / 4, dtype=T, device=dev)
+    W = torch.full((128, 64), 2.0, dtype=T, device=dev)
+    want = torch.full((40, 128), 64 * 2 * tiny / 4, dtype=T, device=dev)
+    assert torch.equal(A.aps_linear(X, W), want) and torch.equal(A.aps_linear(X[:3], W), want[:3])
+    assert torch.equal(A.aps_linear_grad_input(X, W.t().contiguous()), want)
+
+
+def test_rows_in_a_long_buffer(dev):
+    """Operands and outputs whose rows lie beyond 2^31 elements of each other's
+    start: strides of 2^20 and 2100 rows."""
+    ld, M, N, K = 1 << 20, 2100, 96, 64
+    buf = torch.zeros(M * ld, dtype=torch.bfloat16, device=dev)
+    X = buf.view(M, ld)[:, :K]
+    Y = buf.view(M, ld)[:, 1024:1024 + N]
+    X.copy_(torch.randn(M, K, generator=_gen(1)))
+    W = torch.randn(N, K, generator=_gen(2)).to(dev).bfloat16()
+    A.aps_linear(X, W, Y=Y)
+    assert torch.equal(Y, A.aps_linear(X.contiguous(), W))
+    codes = buf.view(torch.uint8).view(M, 2 * ld)[:, 8192:8192 + K]
+    words = torch.empty(66, 1, dtype=torch.int32, device=dev)
+    A.aps_checkpoint_save(X, FMT["1-4-3"], codes, words)
+    rc, rw = A.aps_checkpoint_save(X.contiguous(), FMT["1-4-3"])
+    assert torch.equal(codes, rc) and torch.equal(words, rw)
+    # strides choose the kernel, and with it the sums' order: within the sums' bound
+    dW = A.aps_linear_grad_weight(Y, codes, words, FMT["1-4-3"])
+    x, y = R.load(rc, rw, "1-4-3"), Y.double()
+    ref = y.t() @ x
+    assert bool(((dW.double() - ref).abs() <= R.sums_bound(x.abs(), y.abs().t()) + 2.0 ** -24 * ref.abs()).all())
+    del buf, X, Y, codes
+    torch.cuda.empty_cache()
