@@ -572,7 +572,9 @@ def _fresh(like, size, stream, dtype=None):
     if stream is None:
         return like.new_empty(size, dtype=dtype)
     import torch
-    with torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream):
+    if isinstance(stream, int):  # a hipStream_t; 0 is the default stream
+        stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream(like.device)
+    with torch.cuda.stream(stream):
         return like.new_empty(size, dtype=dtype)
 
 

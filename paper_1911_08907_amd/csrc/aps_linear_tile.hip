@@ -224,24 +224,21 @@ __device__ __forceinline__ typename Mat<T>::frag decode_fragment(i32x2 w, int32_
     typedef Mat<T> M;
     const float inv = pow2_of(-ck_ft(word));
     if constexpr (sizeof(T) == 4) {
-        f32x4 d;
         float z[4];
         ck_decode4<E5>((uint32_t)w[s % 2], inv, word & CK_ODD, z);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) d[i] = z[i];
-        return d;
+        return f32x4{z[0], z[1], z[2], z[3]};
     } else {
-    u4v v = {M::template two<E5, false>(w[0], inv), M::template two<E5, true>(w[0], inv),
-             M::template two<E5, false>(w[1], inv), M::template two<E5, true>(w[1], inv)};
-    if (!E5 && (word & CK_ODD)) {  // the conversion knows no INF of 1-4-3
+        u4v v = {M::template two<E5, false>(w[0], inv), M::template two<E5, true>(w[0], inv),
+                 M::template two<E5, false>(w[1], inv), M::template two<E5, true>(w[1], inv)};
+        if (!E5 && (word & CK_ODD)) {  // the conversion knows no INF of 1-4-3
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t c = ((uint32_t)w[i / 4] >> (i % 4 * 8)) & 0xFFu, sh = i % 2 * 16;
-            const uint32_t x = ((c & 0x80u) << 8) | ((c & 0x7Fu) > 0x78u ? M::NAN_ : M::INF);
-            if ((c & 0x7Fu) >= 0x78u) v[i / 2] = (v[i / 2] & ~(0xFFFFu << sh)) | (x << sh);
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t c = ((uint32_t)w[i / 4] >> (i % 4 * 8)) & 0xFFu, sh = i % 2 * 16;
+                const uint32_t x = ((c & 0x80u) << 8) | ((c & 0x7Fu) > 0x78u ? M::NAN_ : M::INF);
+                if ((c & 0x7Fu) >= 0x78u) v[i / 2] = (v[i / 2] & ~(0xFFFFu << sh)) | (x << sh);
+            }
         }
-    }
-    return __builtin_bit_cast(typename M::frag, v);
+        return __builtin_bit_cast(typename M::frag, v);
     }
 }
 
@@ -329,18 +326,18 @@ __global__ __launch_bounds__(S::THREADS, 2) void k_lin_tile(LinArgs a) {
             word[1] = cld(a.zexps, min(c / CK_ROWS + 1, (int)(a.nc - 1) / CK_ROWS) * nb + pb);
         }
         F p[2][2], q[2][FQ];
-        i32x2 codes[2];
+        // codes stay codes until their step, so that nothing waits for a read
+        // just issued; fp32 has two steps from one read
+        i32x2 codes[2][2];
+        constexpr int per = sizeof(T) == 4 ? 2 : 1;
         const auto read = [&](int s) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                if constexpr (OP == OP_DW)
-                    {
-                    const int g = sizeof(T) == 4 ? s / 2 : s;  // fp32: two steps from one read
-                    if (g == s || s % 2 == 0) codes[i] = RP.read_codes(use, i, g);
-                    p[s & 1][i] = decode_fragment<T, E5>(codes[i], word[sizeof(T) == 4 ? 0 : s / 2], s);
-                }
-                else
+                if constexpr (OP == OP_DW) {
+                    if (s % per == 0) codes[s / per & 1][i] = RP.read_codes(use, i, s / per);
+                } else {
                     p[s & 1][i] = RP.read(use, i, s);
+                }
             }
 #pragma unroll
             for (int j = 0; j < FQ; ++j) q[s & 1][j] = RQ.read(use + OpP::BYTES, j, s);
@@ -354,6 +351,10 @@ __global__ __launch_bounds__(S::THREADS, 2) void k_lin_tile(LinArgs a) {
             for (int n = first(s, OpQ::LOADS); n < first(s + 1, OpQ::LOADS); ++n) Q.load(fill + OpP::BYTES, n, left);
             if (s < 3) read(s + 1);
             __builtin_amdgcn_sched_barrier(0);
+            if constexpr (OP == OP_DW)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    p[s & 1][i] = decode_fragment<T, E5>(codes[s / per & 1][i], word[sizeof(T) == 4 ? 0 : s / 2], s);
 #pragma unroll
             for (int j = 0; j < FQ; ++j)
 #pragma unroll
@@ -397,7 +398,10 @@ __global__ __launch_bounds__(S::THREADS, 2) void k_lin_tile(LinArgs a) {
                 a.dbias[q] = a.accumulate ? a.dbias[q] + sum : sum;
         }
     }
-    __syncthreads();  // the stages are read out
+    // the stages are read out, and the loads behind the contraction's end, which
+    // write zeros, have written them
+    __builtin_amdgcn_s_waitcnt(WAIT_LOADS);
+    __syncthreads();
     int32_t word[FQ] = {};
     if constexpr (OP == OP_FWD) {
         if (a.codes) {

@@ -331,6 +331,21 @@ def test_empty_dimensions(dev, t):
     assert A.aps_checkpoint_load(codes, words, FMT["1-4-3"], dtype=T).shape == (0, 6)
 
 
+@pytest.mark.parametrize("t", list(TYPES))
+@pytest.mark.parametrize("rows", [1000, 1001])
+def test_empty_contractions_of_odd_rows(dev, t, rows):
+    """No row to contract over, and operand rows that would have been copied."""
+    T = TYPES[t]
+    z = lambda *s: torch.zeros(*s, dtype=T, device=dev)  # noqa: E731
+    none = torch.zeros(0, 520, dtype=torch.uint8, device=dev), torch.zeros(0, 5, dtype=torch.int32, device=dev)
+    db = torch.full((rows,), 5.0, device=dev)
+    dW = A.aps_linear_grad_weight(z(0, rows), *none, FMT["1-4-3"], torch.full((rows, 520), 2.0, device=dev), db)
+    assert not bool(dW.any()) and not bool(db.any())
+    r = torch.ones(333, rows, dtype=T, device=dev)
+    assert torch.equal(A.aps_linear_grad_input(z(333, 0), z(0, rows), r), r)
+    assert not bool(A.aps_linear(z(333, 0), z(rows, 0)).any())
+
+
 @pytest.mark.parametrize("M,N,K", [(5, 70, 40), (40, 256, 128), (300, 256, 128), (300, 130, 101)])
 @pytest.mark.parametrize("t", list(TYPES))
 def test_bad_tokens_stay_their_own(dev, t, M, N, K):
@@ -578,6 +593,8 @@ def test_streams_and_workspaces(dev):
     out = torch.empty_like(ref)
     torch.cuda.synchronize()
     A.aps_linear(X, W, b, r, Y=out, stream=streams[0])
+    outs += [A.aps_linear(X, W, b, r, stream=streams[1]), A.aps_linear(X, W, b, r, stream=streams[1].cuda_stream),
+             A.aps_linear(X, W, b, r, stream=0)]
     torch.cuda.synchronize()
     for o in outs + [out]:
         assert torch.equal(o, ref)
