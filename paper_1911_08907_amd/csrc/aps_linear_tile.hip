@@ -23,6 +23,12 @@
 //                two, to the matrix type: exact
 // An fp32 step is 8 c by four instructions of 2: a lane's half h holds 4 c from
 // 16 (s / 2) + 8 h + 4 (s & 1) on in step s, so that two steps are one read of codes.
+//
+// Measured, bf16: 16384 x 1024 x 4096 forward 116 us (1.18 PFLOP/s; the matrix
+// units 55 % busy at the 2.0 GHz that their power leaves), 4096 x 4096 x 1024
+// 37, with GELU and a checkpoint 54; the weight gradient of 16384 x 4096 x 1024 127
+// us in four pieces.  With every load a hit in L2 8192^3 gains 9 %, without LDS
+// reads 5 %: neither alone bounds it.  fp32 4096 x 4096 x 1024 252 us, 136 TFLOP/s.
 // Elements past an operand's end are read as zero by the buffer loads' own
 // range check, through an offset that is out of range.
 #include "aps_linear.hpp"
