@@ -18,8 +18,9 @@
  * dW and db are fp32.  Sums are held in fp32 and a result is rounded once,
  * to nearest even, when it is stored.  Matrices are row-major with a row
  * stride in elements, at least the row's length; pointers are aligned to
- * their element.  Rows aligned to 16 bytes (pointer and stride) and lengths
- * that are multiples of 8 run fastest; no alignment or length is refused.
+ * their element.  Rows of whole 16-byte chunks (8 or 4 elements, 16 codes)
+ * that start on them (pointer and stride) run fastest; no alignment or length
+ * is refused.
  * Sizes: M, N, K in [0, 2^22] with every matrix at most 2^22 blocks of
  * 32 x 128 (2^34 elements); row strides up to 2^31 - 1.  Arrays that a
  * call does not touch (a dimension is 0) may be NULL.

@@ -551,17 +551,21 @@ def _ckpt(codes, ckpt_exp, dev, shape) -> int:
     return ldc
 
 
-def _new_ckpt(M: int, C: int, codes, ckpt_exp, like, stream):
+def _ckpt_out(M: int, C: int, codes, ckpt_exp, like, stream) -> tuple:
+    """A checkpoint's arrays, made here where they are missing, and the codes' row stride."""
+    made = codes is None and ckpt_exp is None
     if codes is None:
         codes = _fresh(like, (M, C), stream, _dtypes(*_U8)[0])
     if ckpt_exp is None:
         ckpt_exp = _fresh(like, _ckpt_words(M, C), stream, _dtypes(*_I32)[0])
-    return codes, ckpt_exp
+    return codes, ckpt_exp, (C or 1) if made else _ckpt(codes, ckpt_exp, like.device, (M, C))
 
 
 def aps_linear_workspace_bytes(op: int, M: int, N: int, K: int, dtype) -> int:
     """Bytes of workspace of aps_linear (APS_LINEAR_FORWARD), aps_linear_grad_input
     or aps_linear_grad_weight; ``dtype`` is a torch dtype."""
+    if dtype not in _dtype_codes():
+        raise ValueError(f"dtype must be float32, bfloat16 or float16, got {dtype}")
     return int(lib().aps_linear_workspace_bytes(int(op), int(M), int(N), int(K), _dtype_codes()[dtype]))
 
 
@@ -618,12 +622,12 @@ def aps_linear(X, W, bias=None, residual=None, act: int = APS_ACT_NONE, Y=None, 
         _need(bias, "bias", T, N, dev)
     ldr = 0 if residual is None else _matrix(residual, "residual", T, dev, (M, N))
     if Y is None:
-        Y = _fresh(X, (M, N), stream)
-    ldy = _matrix(Y, "Y", T, dev, (M, N))
+        Y, ldy = _fresh(X, (M, N), stream), N or 1
+    else:
+        ldy = _matrix(Y, "Y", T, dev, (M, N))
     ldc = 0
     if ckpt_fmt is not None:
-        codes, ckpt_exp = _new_ckpt(M, N, codes, ckpt_exp, X, stream)
-        ldc = _ckpt(codes, ckpt_exp, dev, (M, N))
+        codes, ckpt_exp, ldc = _ckpt_out(M, N, codes, ckpt_exp, X, stream)
     elif codes is not None or ckpt_exp is not None:
         raise ValueError("codes and ckpt_exp need ckpt_fmt")
     ws, nbytes = _linear_workspace(APS_LINEAR_FORWARD, M, N, K, dt, workspace, X, stream)
@@ -647,8 +651,9 @@ def aps_linear_grad_input(dZ, W, residual=None, act: int = APS_ACT_NONE, codes=N
         raise ValueError(f"inner dimensions differ: dZ has {N} columns, W {W.shape[0]} rows")
     ldr = 0 if residual is None else _matrix(residual, "residual", T, dev, (M, K))
     if dX is None:
-        dX = _fresh(dZ, (M, K), stream)
-    ldx = _matrix(dX, "dX", T, dev, (M, K))
+        dX, ldx = _fresh(dZ, (M, K), stream), K or 1
+    else:
+        ldx = _matrix(dX, "dX", T, dev, (M, K))
     ldc = 0
     if int(act) != APS_ACT_NONE:
         if fmt is None:
@@ -678,8 +683,9 @@ def aps_linear_grad_weight(dZ, codes, ckpt_exp, fmt: Format, dW=None, dbias=None
     if dW is None:
         if accumulate:
             raise ValueError("accumulate needs dW")
-        dW = _fresh(dZ, (N, K), stream, _dtypes(*_F32)[0])
-    lddw = _matrix(dW, "dW", _dtypes(*_F32), dev, (N, K))
+        dW, lddw = _fresh(dZ, (N, K), stream, _dtypes(*_F32)[0]), K or 1
+    else:
+        lddw = _matrix(dW, "dW", _dtypes(*_F32), dev, (N, K))
     _need(dbias, "dbias", _dtypes(*_F32), N, dev, optional=True)
     ws, nbytes = _linear_workspace(APS_LINEAR_GRAD_WEIGHT, M, N, K, dt, workspace, dZ, stream)
     _check("aps_linear_grad_weight", lib().aps_linear_grad_weight(
@@ -695,8 +701,9 @@ def aps_activation_grad(dY, codes, ckpt_exp, fmt: Format, act: int, dZ=None, str
     M, C = dY.shape
     ldc = _ckpt(codes, ckpt_exp, dev, (M, C))
     if dZ is None:
-        dZ = _fresh(dY, (M, C), stream)
-    ldz = _matrix(dZ, "dZ", T, dev, (M, C))
+        dZ, ldz = _fresh(dY, (M, C), stream), C or 1
+    else:
+        ldz = _matrix(dZ, "dZ", T, dev, (M, C))
     _check("aps_activation_grad", lib().aps_activation_grad(
         _ptr(dY), ldy, int(act), fmt.c(), _ptr(codes), ldc, _ptr(ckpt_exp), _ptr(dZ), ldz, M, C, dt,
         _stream(stream, dev)))
@@ -708,8 +715,7 @@ def aps_checkpoint_save(X, fmt: Format, codes=None, ckpt_exp=None, stream=None):
     ldx, _, dt = _float_input(X, "X")
     dev = X.device
     M, C = X.shape
-    codes, ckpt_exp = _new_ckpt(M, C, codes, ckpt_exp, X, stream)
-    ldc = _ckpt(codes, ckpt_exp, dev, (M, C))
+    codes, ckpt_exp, ldc = _ckpt_out(M, C, codes, ckpt_exp, X, stream)
     _check("aps_checkpoint_save", lib().aps_checkpoint_save(_ptr(X), ldx, M, C, dt, fmt.c(), _ptr(codes), ldc,
                                                             _ptr(ckpt_exp), _stream(stream, dev)))
     return codes, ckpt_exp
@@ -723,10 +729,11 @@ def aps_checkpoint_load(codes, ckpt_exp, fmt: Format, act: int = APS_ACT_NONE, X
     if X is None:
         if dtype not in _dtype_codes():
             raise ValueError(f"dtype must be float32, bfloat16 or float16, got {dtype}")
-        X = _fresh(codes, (M, C), stream, dtype)
-    elif dtype is not None and X.dtype != dtype:
-        raise ValueError(f"X is of dtype {X.dtype}, not {dtype}")
-    ldx = _matrix(X, "X", _dtype_codes(), dev, (M, C))
+        X, ldx = _fresh(codes, (M, C), stream, dtype), C or 1
+    else:
+        ldx = _matrix(X, "X", _dtype_codes(), dev, (M, C))
+        if dtype is not None and X.dtype != dtype:
+            raise ValueError(f"X is of dtype {X.dtype}, not {dtype}")
     _check("aps_checkpoint_load", lib().aps_checkpoint_load(_ptr(codes), ldc, _ptr(ckpt_exp), M, C, fmt.c(), int(act),
                                                             _ptr(X), ldx, _dtype_codes()[X.dtype],
                                                             _stream(stream, dev)))

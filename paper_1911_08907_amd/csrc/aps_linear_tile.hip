@@ -506,7 +506,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void k_lin_tile(LinArgs a) {
 // where more tiles are at work, their share of the GPU; per tile its epilogue;
 // for a split the join's launch and the partial sums' way out and in.  The
 // terms were fitted to graph replays of 40 products from 64 x 64 x 16384 to
-// 16384 x 4096 x 1024, where the model's choice took at most 1.16 times the best
+// 16384 x 4096 x 1024, where the model's choice took at most 1.17 times the best
 // of all shapes with 1 to 32 pieces (in us: 512 x 4096 x 1024 bf16, small 9.8, middle
 // 12.1, big 27.8; 4096 x 4096 x 1024, small 50.5, middle 43.5, big 36.5; 64 x
 // 1024 x 4096, small in 8 pieces 10.4, in 2 17.7).

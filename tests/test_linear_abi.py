@@ -122,6 +122,25 @@ def test_workspace_bytes(lib):
                 assert w(op, *dims, dt) < 1 << 31
 
 
+def test_tile_kernels_keep_their_sums_in_registers():
+    """No instance of the tile kernel takes scratch: accumulators that spilled
+    in the stage loop ran six times slower."""
+    from tests import test_kernel_resources as TR
+    msgpack = pytest.importorskip("msgpack")
+    if not os.path.exists(A.LIB_PATH):
+        pytest.skip("libaps.so is not built")
+    blob = open(A.LIB_PATH, "rb").read()
+    scratch = {k[".name"]: k[".private_segment_fixed_size"]
+               for elf in TR._code_objects(blob) for k in TR._kernels(elf, msgpack)}
+    tile = {n: v for n, v in scratch.items() if "k_lin_tile" in n}
+    assert len(tile) == 2 * 3 * 2 * 3 + 3 * 2 * 2 and not any(tile.values()), tile
+
+
+def test_workspace_bytes_needs_a_known_type():
+    with pytest.raises(ValueError):
+        A.aps_linear_workspace_bytes(0, 8, 8, 8, torch.float64)
+
+
 def test_binding_refuses_cpu_tensors():
     X, W = torch.zeros(4, 8), torch.zeros(3, 8)
     c, e = torch.zeros(4, 8, dtype=torch.uint8), torch.zeros(1, 1, dtype=torch.int32)
