@@ -43,7 +43,10 @@
  *
  * Activations: none, max(z, 0), z * Phi(z) with the normal distribution's
  * Phi (the exact GELU), z / (1 + exp(-z)); at +-INF their limits.  The
- * derivative of max(z, 0) at 0 is 0.  A NaN gives NaN.
+ * derivative of max(z, 0) at 0 is 0.  A NaN gives NaN.  Of a given z, fp32
+ * results are within 2^-20 of the function relative to themselves (derivatives
+ * to their two terms), 16-bit ones within 2^-14 before they are rounded, as
+ * long as exp(-z^2 / 2) of GELU or exp(-|z|) of SiLU is a normal fp32 number.
  *
  * Streams, errors and status codes are those of aps.h: arguments are checked
  * on the host before anything is enqueued on `stream`, and the contents of

@@ -225,8 +225,8 @@ __global__ __launch_bounds__(CTHREADS) void k_ckpt_load(CkArgs a) {
                 ck_decode4<E5>(CodeVec<E>::word(c[s], g), inv, word & CK_ODD, z);
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    y[4 * g + i] = (T)(GRAD ? (float)x[GRAD ? s : 0][4 * g + i] * act_slope<act.value>(z[i])
-                                            : act_value<act.value>(z[i]));
+                    y[4 * g + i] = (T)(GRAD ? (float)x[GRAD ? s : 0][4 * g + i] * act_slope<act.value, exact_act<T>>(z[i])
+                                            : act_value<act.value, exact_act<T>>(z[i]));
             }
             T* o = (T*)a.out + r * a.ldo + w.col;
             if (VEC && w.have >= E) {

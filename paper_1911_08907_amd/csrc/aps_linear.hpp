@@ -106,53 +106,120 @@ __device__ __forceinline__ void store_some_codes(uint8_t* p, int64_t have, bool 
 //
 // GELU: with h = 1 - Phi(|z|) = erfc(|z| / sqrt 2) / 2,
 //   z Phi(z) = max(z, 0) - |z| h,   Phi(z) + z phi(z) = (z < 0 ? h : 1 - h) + z phi(z)
-// so that both tails keep h's own accuracy.  erfc is Abramowitz and Stegun's
-// 7.1.26, t (a1 + ... + a5 t^4) exp(-x^2) with t = 1 / (1 + p x): its error,
-// 1.5e-7 at most, is that of a couple of fp32 roundings of Phi, and phi is the
-// same exponential.  SiLU: the logistic function by one exponential and one
-// reciprocal.  rcp and exp2 are the hardware's, off by one ulp.
+// so that both tails keep h's relative accuracy.  exp(z^2 / 2) h falls slowly,
+// from 1/2 at 0 like 0.399 / |z|: it is t times a polynomial in t = 1 / (1 + p |z|),
+// whose coefficients were fitted to it over |z| <= 14.5 (beyond, h is below
+// fp32's range), and phi is the same exponential.  SiLU: the logistic function by
+// one exponential and one reciprocal.
+//
+// EXACT, for fp32 results: ten terms, fitted for the least relative error (1.3e-8),
+// the exponent's roundings carried into the exponential, the reciprocal refined:
+// GELU comes out within 3.9e-7 of itself, SiLU 2.8e-7 (over N(0, 1) by norm 3.1e-8
+// and 4.6e-8; z (1 + erf) / 2 in fp32 has 3.7e-8 and loses the lower tail).
+// Otherwise the result is rounded to 16 bits: six terms, as close where h is large
+// (2.2e-7 of h and 1) and within 2.3e-5 relative in the tail, a twentieth of a
+// half's rounding; the exponent's roundings stay, 1e-5 of the result at most.
+// rcp and exp2 are the hardware's, off by one ulp; exp2 takes a result
+// below 2^-126 as zero, so that SiLU below -87.3 (1e-36) is zero.
 //
 // The limits at +-INF are the functions' own: the factor |z|, or z, that would
 // meet a zero is held to where the result is exact already.  NaN stays NaN.
 
+// exp2(y + off) of a small off
+__device__ __forceinline__ float exp2_of(float y, float off) {
+    return __builtin_amdgcn_exp2f(y) * __builtin_fmaf(off, 0.69314718f, 1.0f);
+}
+// 1 / d for d in [1, 2^100]
+__device__ __forceinline__ float rcp_refined(float d) {
+    const float r = __builtin_amdgcn_rcpf(d);
+    return __builtin_fmaf(r, __builtin_fmaf(-d, r, 1.0f), r);
+}
+// |z|, at most lim; NaN stays
+__device__ __forceinline__ float magnitude_to(float z, float lim) {
+    const float a = __builtin_fabsf(z);
+    return a > lim ? lim : a;
+}
+
 struct Tail {
     float h, e;  // 1 - Phi(|z|), exp(-z^2 / 2)
 };
+template <bool EXACT>
 __device__ __forceinline__ Tail normal_tail(float z) {
-    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f * 0.70710678f, __builtin_fabsf(z), 1.0f));
-    const float e = __builtin_amdgcn_exp2f(z * z * -0.72134752f);
-    float y = __builtin_fmaf(0.5f * 1.061405429f, t, 0.5f * -1.453152027f);
-    y = __builtin_fmaf(y, t, 0.5f * 1.421413741f);
-    y = __builtin_fmaf(y, t, 0.5f * -0.284496736f);
-    y = __builtin_fmaf(y, t, 0.5f * 0.254829592f);
-    return {y * t * e, e};
-}
-__device__ __forceinline__ float logistic(float z) {
-    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504f));
+    if constexpr (EXACT) {
+        const float a = magnitude_to(z, 15.0f), s = a * a;  // exp(-15^2 / 2) is zero already
+        const float t = rcp_refined(__builtin_fmaf(0.375f, a, 1.0f));
+        // z^2 / 2 log2(e) = y + off: the square's rounding, the product's, the constant's
+        constexpr float c = 0.721347511f, c_lo = 9.62981517e-09f;
+        const float y = s * -c;
+        const float off = __builtin_fmaf(__builtin_fmaf(a, a, -s), -c, __builtin_fmaf(s, -c_lo, __builtin_fmaf(s, -c, -y)));
+        const float e = exp2_of(y, off);
+        float w = __builtin_fmaf(0.0208993945f, t, -0.134001285f);
+        w = __builtin_fmaf(w, t, 0.344836205f);
+        w = __builtin_fmaf(w, t, -0.424009472f);
+        w = __builtin_fmaf(w, t, 0.215563744f);
+        w = __builtin_fmaf(w, t, -0.0561585128f);
+        w = __builtin_fmaf(w, t, 0.108109742f);
+        w = __builtin_fmaf(w, t, 0.125283062f);
+        w = __builtin_fmaf(w, t, 0.14988403f);
+        w = __builtin_fmaf(w, t, 0.14959307f);
+        return {w * t * e, e};
+    } else {
+        const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3f, __builtin_fabsf(z), 1.0f));
+        const float e = __builtin_amdgcn_exp2f(z * z * -0.72134752f);
+        float w = __builtin_fmaf(-0.0788610998f, t, 0.220412575f);
+        w = __builtin_fmaf(w, t, -0.0207146197f);
+        w = __builtin_fmaf(w, t, 0.14547459f);
+        w = __builtin_fmaf(w, t, 0.1136206f);
+        w = __builtin_fmaf(w, t, 0.120067733f);
+        return {w * t * e, e};
+    }
 }
 
-template <int ACT>
+// The logistic function of z and of -z.
+struct Logistic {
+    float s, u;
+};
+// EXACT: from exp(-|z|), which neither overflows nor cancels.
+template <bool EXACT>
+__device__ __forceinline__ Logistic logistic(float z) {
+    if constexpr (EXACT) {
+        constexpr float c = 1.44269502f, c_lo = 1.92596303e-08f;
+        const float a = magnitude_to(z, 104.0f), y = a * -c;
+        const float e = exp2_of(y, __builtin_fmaf(a, -c_lo, __builtin_fmaf(a, -c, -y)));
+        const float r = rcp_refined(1.0f + e), q = e * r;
+        return {z < 0.0f ? q : r, z < 0.0f ? r : q};
+    } else {
+        const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504f));
+        return {s, 1.0f - s};
+    }
+}
+
+template <int ACT, bool EXACT>
 __device__ __forceinline__ float act_value(float z) {
     if constexpr (ACT == APS_ACT_RELU) return z < 0.0f ? 0.0f : z;
     if constexpr (ACT == APS_ACT_GELU)
-        return __builtin_fmaf(-__builtin_fminf(__builtin_fabsf(z), 15.0f), normal_tail(z).h, __builtin_fmaxf(z, 0.0f));
-    if constexpr (ACT == APS_ACT_SILU) return (z < -104.0f ? -104.0f : z) * logistic(z);
+        return __builtin_fmaf(-__builtin_fminf(__builtin_fabsf(z), 15.0f), normal_tail<EXACT>(z).h, __builtin_fmaxf(z, 0.0f));
+    if constexpr (ACT == APS_ACT_SILU) return (z < -104.0f ? -104.0f : z) * logistic<EXACT>(z).s;
     return z;
 }
 
-template <int ACT>
+template <int ACT, bool EXACT>
 __device__ __forceinline__ float act_slope(float z) {
     if constexpr (ACT == APS_ACT_RELU) return z > 0.0f ? 1.0f : (z != z ? z : 0.0f);
     if constexpr (ACT == APS_ACT_GELU) {
-        const Tail n = normal_tail(z);
+        const Tail n = normal_tail<EXACT>(z);
         return __builtin_fmaf(__builtin_amdgcn_fmed3f(z, -15.0f, 15.0f), n.e * 0.39894228f, z < 0.0f ? n.h : 1.0f - n.h);
     }
     if constexpr (ACT == APS_ACT_SILU) {
-        const float s = logistic(z);
-        return s * __builtin_fmaf(__builtin_amdgcn_fmed3f(z, -104.0f, 104.0f), 1.0f - s, 1.0f);
+        const Logistic l = logistic<EXACT>(z);
+        return l.s * __builtin_fmaf(__builtin_amdgcn_fmed3f(z, -104.0f, 104.0f), l.u, 1.0f);
     }
     return 1.0f;
 }
+
+// whether results of type T take the EXACT form
+template <class T>
+constexpr bool exact_act = sizeof(T) == 4;
 
 // f(std::integral_constant<int, ACT>) of a call's activation: one copy of the
 // code each, chosen once.
@@ -348,7 +415,7 @@ __device__ __forceinline__ void lin_finish(const LinArgs& a, const LinRead<T, OP
         }
         if constexpr (OP == OP_FWD) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = act_value<ACT>(v[i + e]);
+            for (int e = 0; e < 4; ++e) y[e] = act_value<ACT, exact_act<T>>(v[i + e]);
         } else if constexpr (OP == OP_DX) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) y[e] = v[i + e];
@@ -356,7 +423,7 @@ __device__ __forceinline__ void lin_finish(const LinArgs& a, const LinRead<T, OP
                 float z[4];
                 ck_decode4<E5>(in.c[i / 4], pow2_of(-ck_ft(in.word)), in.word & CK_ODD, z);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) y[e] *= act_slope<ACT>(z[e]);
+                for (int e = 0; e < 4; ++e) y[e] *= act_slope<ACT, exact_act<T>>(z[e]);
             }
         }
         if constexpr (OP != OP_DW) {

@@ -1,0 +1,90 @@
+"""The linear layer's calls where they could go wrong unseen by
+tests/test_gpu_linear.py: results relative to themselves, and the forms of a
+call that the header allows."""
+import math
+
+import pytest
+import torch
+
+from paper_1911_08907_amd import aps as A
+from tests import linear_ref as R
+from tests._util import log
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"bf16": torch.bfloat16, "fp16": torch.float16, "fp32": torch.float32}
+FMT = {"1-5-2": A.Format(5, 2), "1-4-3": A.Format(4, 3)}
+ACT = {"none": A.APS_ACT_NONE, "relu": A.APS_ACT_RELU, "gelu": A.APS_ACT_GELU, "silu": A.APS_ACT_SILU}
+
+
+@pytest.fixture(scope="module")
+def dev():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    A.lib()
+    return torch.device("cuda:0")
+
+
+# ------------------------------------------------- activations, relative to themselves
+#
+# fp32, in units of 2^-24: the exponential's and the reciprocal's own ulp (2 and
+# 2), their corrections (2), the polynomial's roundings and fit (4), the products
+# and the last sum (4): within 16.  16 bits: the fit's 2.3e-5 and the exponent's
+# roundings (122, the largest, is rounded by 4e-6, the square before it by 5e-6):
+# within 2^-14, on top of the result's own rounding.
+
+def _relative(T):
+    return 16 * 2.0 ** -24 if T == torch.float32 else 2.0 ** -14 + R.half_step(T)
+
+
+@pytest.mark.parametrize("act", ["gelu", "silu"])
+@pytest.mark.parametrize("t", list(TYPES))
+def test_activations_keep_their_relative_accuracy(dev, t, act):
+    """K = 0: z is the bias itself.  The tails too, as far as exp is a normal
+    number: GELU down to -12.9, SiLU down to -87."""
+    T = TYPES[t]
+    low = -12.9 if act == "gelu" else -87.0
+    z = torch.cat([torch.linspace(low, 13, 6000), torch.linspace(-1, 1, 2192)]).to(T)
+    z = z.clamp(min=math.ceil(low * 8) / 8)
+    ref = R.act(z.double(), act)
+    tol = _relative(T) * ref.abs() + R.tiny(T)
+    none = lambda *s: torch.zeros(*s, dtype=T, device=dev)  # noqa: E731
+    for M in (1, 40):  # the kernels for few rows and for more
+        Y = A.aps_linear(none(M, 0), none(z.numel(), 0), z.to(dev), None, ACT[act]).cpu()
+        err = (Y.double() - ref).abs()
+        assert bool((err <= tol).all()), (M, float(z[(err / tol).argmax() % z.numel()]), float((err / tol).max()))
+
+
+@pytest.mark.parametrize("act", ["gelu", "silu"])
+@pytest.mark.parametrize("fmt", list(FMT))
+@pytest.mark.parametrize("t", list(TYPES))
+def test_slopes_keep_their_accuracy(dev, t, fmt, act):
+    """The derivative at every code: relative to its two terms' magnitudes, which
+    cancel at one place only; through both calls that take it, and the
+    activation of the same values read back."""
+    T = TYPES[t]
+    codes = torch.arange(256, dtype=torch.uint8).repeat(64, 1)
+    words = torch.tensor([[3, 5], [4, 12]], dtype=torch.int32)
+    z = R.load(codes, words, fmt)
+    z = torch.where(torch.isfinite(z), z, 0.0)
+    if act == "gelu":
+        first, second = 0.5 * torch.special.erfc(-z / math.sqrt(2)), z * torch.exp(-z * z / 2) / math.sqrt(2 * math.pi)
+        normal = z > -12.9
+    else:
+        first = 1 / (1 + torch.exp(-z))
+        second = z * first / (1 + torch.exp(z.clamp(max=700)))
+        normal = z > -87.0
+    ref = first + second
+    tol = (_relative(T) - (0 if T == torch.float32 else R.half_step(T))) * (first.abs() + second.abs())
+    tol = tol + (0 if T == torch.float32 else R.half_step(T)) * ref.abs() + R.tiny(T)
+    ok = normal & ((codes & 127) < (0x78 if fmt == "1-4-3" else 0x7C))
+    c, w = codes.to(dev), words.to(dev)
+    one = lambda *s: torch.ones(*s, dtype=T, device=dev)  # noqa: E731
+    for got in (A.aps_activation_grad(one(64, 256), c, w, FMT[fmt], ACT[act]),
+                A.aps_linear_grad_input(one(64, 1), one(1, 256), None, ACT[act], c, w, FMT[fmt])):
+        err = (got.cpu().double() - ref).abs()
+        assert bool((err[ok] <= tol[ok]).all()), float((err / tol)[ok].max())
+    Z = A.aps_checkpoint_load(c, w, FMT[fmt], ACT[act], dtype=T).cpu().double()
+    ref = R.act(z, act)
+    ok &= ref.abs() <= torch.finfo(T).max
+    assert bool(((Z - ref).abs()[ok] <= (_relative(T) * ref.abs() + R.tiny(T))[ok]).all())
