@@ -20,7 +20,7 @@ Dims dims_of(int op, int64_t M, int64_t N, int64_t K) {
 
 int64_t part_stride(int64_t np) { return (np + 3) / 4 * 4; }
 
-enum Kernel { GENERAL, TILE };
+enum Kernel { GENERAL, TILE, DECODE };
 struct Plan {
     Kernel kernel;
     int shape, split;
@@ -38,35 +38,6 @@ int64_t rows_q(int op, const Dims& d) { return op == OP_DW ? d.nc : d.nq; }
 int64_t whole(int64_t n, int64_t chunk) { return (n + chunk - 1) / chunk * chunk; }
 uint64_t copy_bytes(int64_t rows, int64_t row, int chunk) { return (uint64_t)(rows * whole(row, chunk)) * (16 / chunk) + 256; }
 
-// What a call may run, by its sizes alone.
-struct Plans {
-    Plan aligned;  // where operands whose rows are whole chunks also start on them
-    Plan any;
-};
-
-// An operand whose rows are no whole chunks is copied where the models say so:
-// in us, a launch here and there, and its bytes in and out.
-Plans plans_of(int op, const Dims& d, int dtype) {
-    if (d.np == 0 || d.nq == 0) return {{GENERAL, 0, 1, false, false}, {GENERAL, 0, 1, false, false}};
-    const bool f32 = dtype == APS_DTYPE_F32;
-    const int cp = chunk_p(op, dtype), cq = chunk_q(dtype);
-    const bool copy_p = d.nc > 0 && row_p(op, d) % cp != 0, copy_q = d.nc > 0 && row_q(op, d) % cq != 0;
-    const LinTile g = lin_general(op, d.np, d.nq, d.nc, f32);
-    const Plan any{GENERAL, 0, g.split, false, false};
-    // a stage's offsets within a tile fit 31 bits, a copy's threads a launch
-    const int64_t most = (int64_t)1 << 32;
-    if (row_p(op, d) >= (1 << 21) || row_q(op, d) >= (1 << 21) || (copy_p && rows_p(op, d) * row_p(op, d) > most) ||
-        (copy_q && rows_q(op, d) * row_q(op, d) > most))
-        return {any, any};
-    const LinTile t = lin_tile(op, d.np, d.nq, d.nc, f32);
-    double us = t.us;
-    if (copy_p || copy_q) us += 6.0;
-    if (copy_p) us += (double)copy_bytes(rows_p(op, d), row_p(op, d), cp) / 1.5e6;
-    if (copy_q) us += (double)copy_bytes(rows_q(op, d), row_q(op, d), cq) / 1.5e6;
-    if ((copy_p || copy_q) && us >= g.us) return {any, any};
-    return {{TILE, t.shape, t.split, copy_p, copy_q}, any};
-}
-
 // Partial sums, then the copies.
 uint64_t part_bytes(int op, const Dims& d, int split) {
     return split > 1 ? ((uint64_t)(split * d.nq * (part_stride(d.np) + (op == OP_DW ? 1 : 0))) * 4 + 255) / 256 * 256 : 0;
@@ -77,25 +48,82 @@ uint64_t bytes_of(int op, const Dims& d, int dtype, const Plan& p) {
            (p.copy_q ? copy_bytes(rows_q(op, d), row_q(op, d), chunk_q(dtype)) : 0);
 }
 
-uint64_t workspace_of(int op, const Dims& d, int dtype, const Plans& p) {
-    return std::max(bytes_of(op, d, dtype, p.aligned), bytes_of(op, d, dtype, p.any));
-}
+// The kernels' choices for a call's sizes, and from them what it runs.
+class Planner {
+  public:
+    Planner(int op, const Dims& d, int dtype) : op_(op), d_(d), dtype_(dtype) {
+        empty_ = d.np == 0 || d.nq == 0;
+        if (empty_) return;
+        const bool f32 = dtype == APS_DTYPE_F32;
+        general_ = lin_general(op, d.np, d.nq, d.nc, f32);
+        // a stage's offsets within a tile fit 31 bits
+        tile_fits_ = row_p(op, d) < (1 << 21) && row_q(op, d) < (1 << 21);
+        if (tile_fits_) tile_ = lin_tile(op, d.np, d.nq, d.nc, f32);
+    }
+
+    // The kernel that reads anything, from any workspace that a call is asked for.
+    Plan any() const { return {GENERAL, 0, empty_ ? 1 : general_.split, false, false}; }
+
+    // What the models say is fastest where the operands' rows do (on_p, on_q) or
+    // do not start on 16-byte chunks; keeps: the call keeps a checkpoint of z.
+    Plan plan(bool keeps, bool on_p, bool on_q) const {
+        if (empty_) return any();
+        const bool f32 = dtype_ == APS_DTYPE_F32, rows = d_.nc > 0;
+        // operands that the tile kernel would have to read from copies
+        const bool copy_p = rows && !whole_p(), copy_q = rows && !whole_q();
+        const bool off = rows && ((whole_p() && !on_p) || (whole_q() && !on_q));
+        // a copy's threads fit a launch
+        const int64_t most = (int64_t)1 << 32;
+        const bool tile = tile_fits_ && !off && !(copy_p && rows_p(op_, d_) * row_p(op_, d_) > most) &&
+                          !(copy_q && rows_q(op_, d_) * row_q(op_, d_) > most);
+        const bool few = op_ == OP_FWD && !keeps && d_.nq <= LIN_FEW;
+        double us = 1e300;
+        Plan best = any();
+        if (tile) {
+            us = tile_.us;
+            best = {TILE, tile_.shape, tile_.split, copy_p, copy_q};
+        }
+        if (copy_p || copy_q || !tile) {
+            if (copy_p || copy_q) us += lin_align_us((copy_p ? copy_bytes(rows_p(op_, d_), row_p(op_, d_), chunk_p(op_, dtype_)) : 0) +
+                                                     (copy_q ? copy_bytes(rows_q(op_, d_), row_q(op_, d_), chunk_q(dtype_)) : 0));
+            if (us >= general_.us) us = general_.us, best = any();
+        }
+        if (few) {
+            // few rows leave the others no faster than the weights come from memory
+            us = std::max(us, 3.0 + (double)d_.np * d_.nc * lin_elem_bytes(dtype_) / 3.6e6);
+            if (lin_decode_us(d_.np, d_.nq, d_.nc, f32, !(copy_p || copy_q || off)) <= us) best = {DECODE, 0, 1, false, false};
+        }
+        return best;
+    }
+
+    // Bytes that suffice for every call.
+    uint64_t need() const {
+        return std::max(bytes_of(op_, d_, dtype_, plan(true, true, true)), bytes_of(op_, d_, dtype_, any()));
+    }
+
+  private:
+    bool whole_p() const { return row_p(op_, d_) % chunk_p(op_, dtype_) == 0; }
+    bool whole_q() const { return row_q(op_, d_) % chunk_q(dtype_) == 0; }
+    int op_;
+    Dims d_;
+    int dtype_;
+    bool empty_, tile_fits_ = false;
+    LinTile general_{}, tile_{};
+};
 
 // A pointer and stride on whole chunks, for an operand that is read in place.
 bool on_chunks(const void* p, int64_t ld, int chunk) { return aligned16(p) && ld % chunk == 0 && ld < (1 << 21); }
+bool on_chunks_p(int op, int dtype, const LinArgs& a) { return on_chunks(a.P, a.ldp, chunk_p(op, dtype)); }
+bool on_chunks_q(int dtype, const LinArgs& a) { return on_chunks(a.Q, a.ldq, chunk_q(dtype)); }
 
-int launch_product(int op, int dtype, bool e5, LinArgs& a, const Plans& plans, void* workspace, hipStream_t s) {
+int launch_product(int op, int dtype, bool e5, LinArgs& a, const Plan& plan, void* workspace, hipStream_t s) {
     const Dims d{a.np, a.nq, a.nc};
     const int cp = chunk_p(op, dtype), cq = chunk_q(dtype);
-    const bool in_place_p = on_chunks(a.P, a.ldp, cp), in_place_q = on_chunks(a.Q, a.ldq, cq);
-    if (op == OP_FWD && !a.codes && a.nq <= LIN_FEW) {
-        a.split = 1;
-        launch_lin_decode(dtype, in_place_p && in_place_q && a.nc % cq == 0, a, s);
+    a.split = plan.split;
+    if (plan.kernel == DECODE) {
+        launch_lin_decode(dtype, on_chunks_p(op, dtype, a) && on_chunks_q(dtype, a) && a.nc % cq == 0, a, s);
         return launched();
     }
-    const bool aligned = (in_place_p || row_p(op, d) % cp != 0) && (in_place_q || row_q(op, d) % cq != 0);
-    const Plan& plan = aligned ? plans.aligned : plans.any;
-    a.split = plan.split;
     a.piece = ((a.nc + a.split - 1) / a.split + 63) / 64 * 64;
     if (a.split > 1) {
         a.ldpart = part_stride(a.np);
@@ -124,12 +152,18 @@ int launch_product(int op, int dtype, bool e5, LinArgs& a, const Plans& plans, v
     return launched();
 }
 
-int check_workspace(int op, const Dims& d, int dtype, const Plans& p, const void* w, uint64_t bytes) {
-    const uint64_t need = workspace_of(op, d, dtype, p);
-    if (need == 0) return APS_OK;
-    if (!w) return APS_ERR_NULL;
-    if (bytes < need) return APS_ERR_SIZE;
-    return aligned16(w) ? APS_OK : APS_ERR_ALIGN;
+// The plan of a call that has `bytes` of workspace at w.
+int choose(int op, int dtype, const LinArgs& a, const void* w, uint64_t bytes, Plan& plan) {
+    const Dims d{a.np, a.nq, a.nc};
+    const Planner planner(op, d, dtype);
+    plan = planner.plan(a.codes != nullptr, on_chunks_p(op, dtype, a), on_chunks_q(dtype, a));
+    const uint64_t need = planner.need();
+    if (need > 0) {
+        if (!w) return APS_ERR_NULL;
+        if (bytes < need) return APS_ERR_SIZE;
+        if (!aligned16(w)) return APS_ERR_ALIGN;
+    }
+    return APS_OK;
 }
 
 }  // namespace
@@ -140,8 +174,7 @@ using namespace aps;
 
 extern "C" uint64_t aps_linear_workspace_bytes(int32_t op, int32_t M, int32_t N, int32_t K, int32_t dtype) {
     if (op < OP_FWD || op > OP_DW || lin_check_dims(M, N, K, dtype) != APS_OK) return 0;
-    const Dims d = dims_of(op, M, N, K);
-    return workspace_of(op, d, dtype, plans_of(op, d, dtype));
+    return Planner(op, dims_of(op, M, N, K), dtype).need();
 }
 
 extern "C" int aps_linear(const void* X, int64_t ldx, const void* W, int64_t ldw, const void* bias, const void* R,
@@ -159,9 +192,6 @@ extern "C" int aps_linear(const void* X, int64_t ldx, const void* W, int64_t ldw
     bool e5 = false;
     if (codes || ckpt_exp) APS_LIN_TRY(lin_check_checkpoint(ckpt_fmt, codes, ldc, ckpt_exp, M, N, e5));
     const Dims d = dims_of(OP_FWD, M, N, K);
-    const Plans plans = plans_of(OP_FWD, d, dtype);
-    APS_LIN_TRY(check_workspace(OP_FWD, d, dtype, plans, workspace, workspace_bytes));
-    if (M == 0 || N == 0) return APS_OK;
     LinArgs a{};
     a.P = W, a.ldp = ldw, a.Q = X, a.ldq = ldx;
     a.np = d.np, a.nq = d.nq, a.nc = d.nc;
@@ -169,7 +199,10 @@ extern "C" int aps_linear(const void* X, int64_t ldx, const void* W, int64_t ldw
     a.codes = codes, a.ldcodes = ldc, a.exps = ckpt_exp, a.act = act;
     a.vec = (rows_of_four(Y, ldy, es) ? LV_OUT : 0) | (rows_of_four(R, ldr, es) ? LV_R : 0) |
             (rows_of_four(codes, ldc, 1) ? LV_CODES : 0) | (lin_aligned(bias, 4 * es) ? LV_BIAS : 0);
-    return launch_product(OP_FWD, dtype, e5, a, plans, workspace, (hipStream_t)stream);
+    Plan plan;
+    APS_LIN_TRY(choose(OP_FWD, dtype, a, workspace, workspace_bytes, plan));
+    if (M == 0 || N == 0) return APS_OK;
+    return launch_product(OP_FWD, dtype, e5, a, plan, workspace, (hipStream_t)stream);
 }
 
 extern "C" int aps_linear_grad_input(const void* dZ, int64_t lddz, const void* W, int64_t ldw, const void* R,
@@ -186,9 +219,6 @@ extern "C" int aps_linear_grad_input(const void* dZ, int64_t lddz, const void* W
     bool e5 = false;
     if (act != APS_ACT_NONE) APS_LIN_TRY(lin_check_checkpoint(fmt, codes, ldc, ckpt_exp, M, K, e5));
     const Dims d = dims_of(OP_DX, M, N, K);
-    const Plans plans = plans_of(OP_DX, d, dtype);
-    APS_LIN_TRY(check_workspace(OP_DX, d, dtype, plans, workspace, workspace_bytes));
-    if (M == 0 || K == 0) return APS_OK;
     LinArgs a{};
     a.P = W, a.ldp = ldw, a.Q = dZ, a.ldq = lddz;
     a.np = d.np, a.nq = d.nq, a.nc = d.nc;
@@ -196,7 +226,10 @@ extern "C" int aps_linear_grad_input(const void* dZ, int64_t lddz, const void* W
     if (act != APS_ACT_NONE) a.zc = codes, a.ldzc = ldc, a.zexps = ckpt_exp;
     a.vec = (rows_of_four(dX, lddx, es) ? LV_OUT : 0) | (rows_of_four(R, ldr, es) ? LV_R : 0) |
             (rows_of_four(codes, ldc, 1) ? LV_ZC : 0);
-    return launch_product(OP_DX, dtype, e5, a, plans, workspace, (hipStream_t)stream);
+    Plan plan;
+    APS_LIN_TRY(choose(OP_DX, dtype, a, workspace, workspace_bytes, plan));
+    if (M == 0 || K == 0) return APS_OK;
+    return launch_product(OP_DX, dtype, e5, a, plan, workspace, (hipStream_t)stream);
 }
 
 extern "C" int aps_linear_grad_weight(const void* dZ, int64_t lddz, aps_format fmt, const uint8_t* codes, int64_t ldc,
@@ -213,14 +246,14 @@ extern "C" int aps_linear_grad_weight(const void* dZ, int64_t lddz, aps_format f
     if (db && K == 0) return APS_ERR_SIZE;  // db is summed beside dW
     if (db && !lin_aligned(db, 4)) return APS_ERR_ALIGN;
     const Dims d = dims_of(OP_DW, M, N, K);
-    const Plans plans = plans_of(OP_DW, d, dtype);
-    APS_LIN_TRY(check_workspace(OP_DW, d, dtype, plans, workspace, workspace_bytes));
-    if (N == 0 || K == 0) return APS_OK;
     LinArgs a{};
     a.P = codes, a.ldp = ldc, a.Q = dZ, a.ldq = lddz;
     a.np = d.np, a.nq = d.nq, a.nc = d.nc;
     a.out = dW, a.ldo = lddw, a.zexps = ckpt_exp, a.dbias = db;
     a.accumulate = flags & APS_GRAD_ACCUMULATE;
     a.vec = rows_of_four(dW, lddw, 4) ? LV_OUT : 0;
-    return launch_product(OP_DW, dtype, e5, a, plans, workspace, (hipStream_t)stream);
+    Plan plan;
+    APS_LIN_TRY(choose(OP_DW, dtype, a, workspace, workspace_bytes, plan));
+    if (N == 0 || K == 0) return APS_OK;
+    return launch_product(OP_DW, dtype, e5, a, plan, workspace, (hipStream_t)stream);
 }

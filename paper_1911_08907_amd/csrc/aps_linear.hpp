@@ -520,8 +520,10 @@ static inline int lin_check_checkpoint(aps_format f, const void* codes, int64_t 
 void launch_lin_general(int op, int dtype, bool e5, const LinArgs& a, hipStream_t s);
 void launch_lin_join(int op, int dtype, bool e5, const LinArgs& a, hipStream_t s);
 
-constexpr int LIN_FEW = 32;  // rows that the decode kernel takes
+constexpr int LIN_FEW = 32;  // rows that the decode kernel takes at most
 void launch_lin_decode(int dtype, bool fast, const LinArgs& a, hipStream_t s);
+// Its time in us; fast: rows of whole chunks that start on them.
+double lin_decode_us(int64_t np, int64_t nq, int64_t nc, bool f32, bool fast);
 
 // One operand's copy into aligned rows (src NULL: none).
 struct LinCopy {
@@ -531,6 +533,7 @@ struct LinCopy {
     int32_t elem;                  // bytes
 };
 void launch_lin_align(const LinCopy& p, const LinCopy& q, hipStream_t s);
+double lin_align_us(uint64_t bytes);  // of copies that take `bytes`
 
 // A choice for an output and a contraction: the tile kernel's shape, the pieces
 // of the contraction, and the model's time in us.

@@ -98,6 +98,30 @@ __global__ __launch_bounds__(64 * DWAVES) void k_lin_decode(LinArgs a) {
 
 }  // namespace
 
+// A launch; then the larger of a workgroup's 4 KB of each weight row after
+// another, whose latency grows with the rows of q, the workgroups' shares of the
+// memory's rate, and a workgroup's start.  Element by element (off chunks) all of
+// it costs more.  Fitted to graph replays of 220 products beside the other
+// kernels, whose faster one the choice then missed by 5 % on average.  In us, this
+// kernel and the best of the others:
+//                            1 row         8             32
+//   4096 x 1024 bf16         4.8, 8.3      4.8, 8.2      6.1, 8.9
+//   ... off chunks           12.3, 9.7     16.0, 9.9     25.1, 11.3
+//   16384 x 4096 bf16, HBM   28.4, 30.6    32.8, 40.1    54.8, 41.4
+//   16384 x 4096 fp32, HBM   62.4, 93.8    67.6, 93.4    113.6, 95.3
+//   1024 x 4096 bf16         7.3, 8.3      8.7, 9.1      14.0, 10.4
+//   16 x 16384 bf16          19.9, 10.7    25.2, 11.7    44.0, 15.0
+double lin_decode_us(int64_t np, int64_t nq, int64_t nc, bool f32, bool fast) {
+    static const struct {
+        double launch, round, per_q, share, share_q;
+    } on[] = {{3.3, 2.05, 0.095, 0.0122, 0.0004}, {3.3, 2.4, 0.1, 0.0142, 0.0004}},
+      off[] = {{7.0, 11.0, 0.55, 0.067, 0.0024}, {7.0, 6.0, 0.33, 0.04, 0.0013}};
+    const auto& m = (fast ? on : off)[f32];
+    const double rounds = (double)nc * (f32 ? 4 : 2) / 4096, groups = (double)((np + DP - 1) / DP);
+    const double work = rounds * std::max(m.round + m.per_q * nq, groups * (m.share + m.share_q * nq));
+    return m.launch + std::max(work, 0.012 * (groups - 128));
+}
+
 void launch_lin_decode(int dtype, bool fast, const LinArgs& a, hipStream_t s) {
     const dim3 grid((unsigned)((a.np + DP - 1) / DP)), block(64 * DWAVES);
     const auto go = [&](auto t) {

@@ -88,3 +88,49 @@ def test_slopes_keep_their_accuracy(dev, t, fmt, act):
     ref = R.act(z, act)
     ok &= ref.abs() <= torch.finfo(T).max
     assert bool(((Z - ref).abs()[ok] <= (_relative(T) * ref.abs() + R.tiny(T))[ok]).all())
+
+
+# ------------------------------------------------- the choice of the kernel
+
+def _bounds(X, W, b=None):
+    """(X W^T + b in float64, a bound of a sum's error in fp32)."""
+    X, W = X.double(), W.double()
+    z = X @ W.t() + (0 if b is None else b.double())
+    return z, R.sums_bound(W.abs().t(), X.abs(), 0 if b is None else b.double().abs())
+
+
+def _random(dev, T, *shapes):
+    g = torch.Generator(device=dev)
+    g.manual_seed(sum(sum(s) for s in shapes))
+    return [torch.randn(*s, generator=g, device=dev).to(T) for s in shapes]
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 16, 16384), (8, 64, 65536), (32, 256, 16384)])
+@pytest.mark.parametrize("t", list(TYPES))
+def test_few_rows_of_a_long_contraction_are_split(dev, t, M, N, K):
+    """Where 16 features to a workgroup leave most of the GPU idle, few rows are
+    summed in pieces as they are with a checkpoint: the same bits."""
+    T = TYPES[t]
+    X, W = _random(dev, T, (M, K), (N, K))
+    log("few rows", t, M, N, K)
+    Y = A.aps_linear(X, W)
+    assert torch.equal(Y, A.aps_linear(X, W, ckpt_fmt=FMT["1-4-3"])[0])
+    z, e = _bounds(X, W)
+    assert bool(((Y.double() - z).abs() <= e + R.half_step(T) * (z.abs() + e) + R.tiny(T)).all())
+
+
+@pytest.mark.parametrize("off", [0, 1])
+@pytest.mark.parametrize("M", [1, 8, 17, 32])
+@pytest.mark.parametrize("t", list(TYPES))
+def test_few_rows_on_and_off_their_chunks(dev, t, M, off):
+    """Every kernel that few rows can take."""
+    T = TYPES[t]
+    for N, K in ((16, 24), (40, 1001), (333, 4096), (2048, 64), (1024, 2000), (5000, 72)):
+        log("few rows", t, M, N, K, off)
+        x, w, b, r = _random(dev, T, (M * K + off,), (N * K + off,), (N,), (M, N))
+        X, W = x[off:].view(M, K), w[off:].view(N, K)
+        Y = A.aps_linear(X, W, b, r, ACT["relu"])
+        z, e = _bounds(X, W, b)
+        ref = z.clamp(min=0) + r.double()
+        e = e + 2.0 ** -24 * ref.abs()
+        assert bool(((Y.double() - ref).abs() <= e + R.half_step(T) * (ref.abs() + e) + R.tiny(T)).all())
