@@ -68,6 +68,7 @@ extern "C" {
 enum { APS_DTYPE_F32 = 0, APS_DTYPE_BF16 = 1, APS_DTYPE_F16 = 2 };
 enum { APS_ACT_NONE = 0, APS_ACT_RELU = 1, APS_ACT_GELU = 2, APS_ACT_SILU = 3 };
 enum { APS_LINEAR_FORWARD = 0, APS_LINEAR_GRAD_INPUT = 1, APS_LINEAR_GRAD_WEIGHT = 2 };
+enum { APS_LINEAR_ON_CHUNKS = 4, APS_LINEAR_NO_CKPT = 8 }; /* aps_linear_workspace_bytes: added to op */
 #define APS_CKPT_ROWS 32
 #define APS_CKPT_COLS 128
 #define APS_CKPT_MAX_EXP 96
@@ -77,8 +78,14 @@ enum { APS_LINEAR_FORWARD = 0, APS_LINEAR_GRAD_INPUT = 1, APS_LINEAR_GRAD_WEIGHT
  * Bytes of workspace that aps_linear (op APS_LINEAR_FORWARD),
  * aps_linear_grad_input or aps_linear_grad_weight needs for a layer with M
  * rows, N out and K in features: the partial sums of a contraction that is
- * split over the GPU.  0 where the call needs none, and for arguments out of
- * range.  Host-only.
+ * split over the GPU, and copies of operands whose rows are no whole 16-byte
+ * chunks.  They suffice for every such call, and a workspace that is given
+ * holds at least as many.  0 where none needs any, and for arguments out of
+ * range.  Host-only.  Flags can be added to op:
+ *   APS_LINEAR_ON_CHUNKS  of operands whose rows start on 16-byte chunks, or
+ *                         are no whole ones: 0 where their call uses none; it
+ *                         can then be made with workspace NULL and 0 bytes
+ *   APS_LINEAR_NO_CKPT    of aps_linear without codes
  */
 uint64_t aps_linear_workspace_bytes(int32_t op, int32_t M, int32_t N, int32_t K, int32_t dtype);
 
@@ -91,7 +98,8 @@ uint64_t aps_linear_workspace_bytes(int32_t op, int32_t M, int32_t N, int32_t K,
  *   codes      uint8 [M][ldc] out with ckpt_exp out, or NULL (then ckpt_fmt is
  *              not read)
  *   workspace  at least aps_linear_workspace_bytes(APS_LINEAR_FORWARD, ...)
- *              bytes, 16-byte aligned; calls that share one must not overlap
+ *              bytes, 16-byte aligned; calls that share one must not overlap.
+ *              NULL with 0 bytes where the call uses none
  * K = 0 gives z = b.
  */
 int aps_linear(const void* X, int64_t ldx, const void* W, int64_t ldw, const void* bias,

@@ -58,6 +58,8 @@ APS_ACT_SILU = 3
 APS_LINEAR_FORWARD = 0
 APS_LINEAR_GRAD_INPUT = 1
 APS_LINEAR_GRAD_WEIGHT = 2
+APS_LINEAR_ON_CHUNKS = 4
+APS_LINEAR_NO_CKPT = 8
 APS_CKPT_ROWS = 32
 APS_CKPT_COLS = 128
 APS_CKPT_MAX_EXP = 96
@@ -563,7 +565,8 @@ def _ckpt_out(M: int, C: int, codes, ckpt_exp, like, stream) -> tuple:
 
 def aps_linear_workspace_bytes(op: int, M: int, N: int, K: int, dtype) -> int:
     """Bytes of workspace of aps_linear (APS_LINEAR_FORWARD), aps_linear_grad_input
-    or aps_linear_grad_weight; ``dtype`` is a torch dtype."""
+    or aps_linear_grad_weight, with APS_LINEAR_ON_CHUNKS or APS_LINEAR_NO_CKPT
+    added or not; ``dtype`` is a torch dtype."""
     if dtype not in _dtype_codes():
         raise ValueError(f"dtype must be float32, bfloat16 or float16, got {dtype}")
     return int(lib().aps_linear_workspace_bytes(int(op), int(M), int(N), int(K), _dtype_codes()[dtype]))
@@ -587,14 +590,24 @@ def _linear_need(op: int, M: int, N: int, K: int, dtype: int) -> int:
     return int(lib().aps_linear_workspace_bytes(op, M, N, K, dtype))
 
 
-def _linear_workspace(op: int, M: int, N: int, K: int, dtype: int, workspace, like, stream):
-    """(tensor, bytes) of the call's workspace; allocated where it is missing and needed."""
+def _off_chunks(t, ld: int) -> bool:
+    """Whether rows of whole 16-byte chunks do not all start on them, or further
+    apart than the library's tiles take."""
+    each = t.element_size()
+    return t.shape[1] * each & 15 == 0 and ((t.data_ptr() | ld * each) & 15 != 0 or ld >= 1 << 21)
+
+
+def _linear_workspace(op: int, M: int, N: int, K: int, dtype: int, workspace, Q, ldq: int, P, ldp: int, stream):
+    """(tensor, bytes) of the workspace of a product of Q and P; allocated where
+    it is missing and needed."""
     if workspace is None:
+        if not (_off_chunks(Q, ldq) or _off_chunks(P, ldp)):
+            op |= APS_LINEAR_ON_CHUNKS
         need = _linear_need(op, M, N, K, dtype)
         if need == 0:
             return None, 0
-        return _fresh(like, need, stream, _dtypes(*_U8)[0]), need
-    _need(workspace, "workspace", _dtypes(*_U8), 0, like.device)
+        return _fresh(Q, need, stream, _dtypes(*_U8)[0]), need
+    _need(workspace, "workspace", _dtypes(*_U8), 0, Q.device)
     return workspace, workspace.numel()
 
 
@@ -630,7 +643,8 @@ def aps_linear(X, W, bias=None, residual=None, act: int = APS_ACT_NONE, Y=None, 
         codes, ckpt_exp, ldc = _ckpt_out(M, N, codes, ckpt_exp, X, stream)
     elif codes is not None or ckpt_exp is not None:
         raise ValueError("codes and ckpt_exp need ckpt_fmt")
-    ws, nbytes = _linear_workspace(APS_LINEAR_FORWARD, M, N, K, dt, workspace, X, stream)
+    op = APS_LINEAR_FORWARD if ckpt_fmt is not None else APS_LINEAR_FORWARD | APS_LINEAR_NO_CKPT
+    ws, nbytes = _linear_workspace(op, M, N, K, dt, workspace, X, ldx, W, ldw, stream)
     _check("aps_linear", lib().aps_linear(
         _ptr(X), ldx, _ptr(W), ldw, _ptr(bias), _ptr(residual), ldr, _ptr(Y), ldy, M, N, K, dt, int(act),
         _NO_FORMAT if ckpt_fmt is None else ckpt_fmt.c(), _ptr(codes), ldc, _ptr(ckpt_exp), _ptr(ws), nbytes,
@@ -661,7 +675,7 @@ def aps_linear_grad_input(dZ, W, residual=None, act: int = APS_ACT_NONE, codes=N
         ldc = _ckpt(codes, ckpt_exp, dev, (M, K))
     elif codes is not None or ckpt_exp is not None or fmt is not None:
         raise ValueError("a checkpoint is read for an activation's derivative only: act is none")
-    ws, nbytes = _linear_workspace(APS_LINEAR_GRAD_INPUT, M, N, K, dt, workspace, dZ, stream)
+    ws, nbytes = _linear_workspace(APS_LINEAR_GRAD_INPUT, M, N, K, dt, workspace, dZ, ldz, W, ldw, stream)
     _check("aps_linear_grad_input", lib().aps_linear_grad_input(
         _ptr(dZ), ldz, _ptr(W), ldw, _ptr(residual), ldr, int(act), _NO_FORMAT if fmt is None else fmt.c(),
         _ptr(codes), ldc, _ptr(ckpt_exp), _ptr(dX), ldx, M, N, K, dt, _ptr(ws), nbytes, _stream(stream, dev)))
@@ -687,7 +701,7 @@ def aps_linear_grad_weight(dZ, codes, ckpt_exp, fmt: Format, dW=None, dbias=None
     else:
         lddw = _matrix(dW, "dW", _dtypes(*_F32), dev, (N, K))
     _need(dbias, "dbias", _dtypes(*_F32), N, dev, optional=True)
-    ws, nbytes = _linear_workspace(APS_LINEAR_GRAD_WEIGHT, M, N, K, dt, workspace, dZ, stream)
+    ws, nbytes = _linear_workspace(APS_LINEAR_GRAD_WEIGHT, M, N, K, dt, workspace, dZ, ldz, codes, ldc, stream)
     _check("aps_linear_grad_weight", lib().aps_linear_grad_weight(
         _ptr(dZ), ldz, fmt.c(), _ptr(codes), ldc, _ptr(ckpt_exp), _ptr(dW), lddw, _ptr(dbias), M, N, K, dt,
         APS_GRAD_ACCUMULATE if accumulate else 0, _ptr(ws), nbytes, _stream(stream, dev)))

@@ -158,7 +158,8 @@ int choose(int op, int dtype, const LinArgs& a, const void* w, uint64_t bytes, P
     const Planner planner(op, d, dtype);
     plan = planner.plan(a.codes != nullptr, on_chunks_p(op, dtype, a), on_chunks_q(dtype, a));
     const uint64_t need = planner.need();
-    if (need > 0) {
+    const bool none = !w && bytes == 0;
+    if (need > 0 && !(none && bytes_of(op, d, dtype, plan) == 0)) {
         if (!w) return APS_ERR_NULL;
         if (bytes < need) return APS_ERR_SIZE;
         if (!aligned16(w)) return APS_ERR_ALIGN;
@@ -173,8 +174,12 @@ int choose(int op, int dtype, const LinArgs& a, const void* w, uint64_t bytes, P
 using namespace aps;
 
 extern "C" uint64_t aps_linear_workspace_bytes(int32_t op, int32_t M, int32_t N, int32_t K, int32_t dtype) {
+    const bool on = op & APS_LINEAR_ON_CHUNKS, keeps = !(op & APS_LINEAR_NO_CKPT);
+    op &= ~(APS_LINEAR_ON_CHUNKS | APS_LINEAR_NO_CKPT);
     if (op < OP_FWD || op > OP_DW || lin_check_dims(M, N, K, dtype) != APS_OK) return 0;
-    return Planner(op, dims_of(op, M, N, K), dtype).need();
+    const Dims d = dims_of(op, M, N, K);
+    const Planner planner(op, d, dtype);
+    return on && bytes_of(op, d, dtype, planner.plan(keeps, true, true)) == 0 ? 0 : planner.need();
 }
 
 extern "C" int aps_linear(const void* X, int64_t ldx, const void* W, int64_t ldw, const void* bias, const void* R,

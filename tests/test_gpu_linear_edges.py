@@ -134,3 +134,52 @@ def test_few_rows_on_and_off_their_chunks(dev, t, M, off):
         ref = z.clamp(min=0) + r.double()
         e = e + 2.0 ** -24 * ref.abs()
         assert bool(((Y.double() - ref).abs() <= e + R.half_step(T) * (ref.abs() + e) + R.tiny(T)).all())
+
+
+# ------------------------------------------------- workspaces
+
+BARE = A.APS_LINEAR_FORWARD | A.APS_LINEAR_ON_CHUNKS | A.APS_LINEAR_NO_CKPT
+
+def _raw(X, W, Y, ws=None, nbytes=0, codes=None, exps=None):
+    M, K = X.shape
+    N = W.shape[0]
+    dt = {torch.float32: A.APS_DTYPE_F32, torch.bfloat16: A.APS_DTYPE_BF16, torch.float16: A.APS_DTYPE_F16}[X.dtype]
+    p = lambda v: None if v is None else v.data_ptr()  # noqa: E731
+    return A.lib().aps_linear(p(X), X.stride(0), p(W), W.stride(0), None, None, 0, p(Y), N, M, N, K, dt, 0,
+                              FMT["1-4-3"].c(), p(codes), N, p(exps), p(ws), nbytes,
+                              torch.cuda.current_stream().cuda_stream)
+
+
+@pytest.mark.parametrize("t", list(TYPES))
+def test_few_rows_need_no_workspace(dev, t):
+    """A call that uses none is made without, and the binding allocates none; one
+    whose contraction is split is not."""
+    T = TYPES[t]
+    M, N, K = 1, 4096, 1024
+    X, W = _random(dev, T, (M, K), (N, K))
+    assert A.aps_linear_workspace_bytes(A.APS_LINEAR_FORWARD, M, N, K, T) > 0
+    assert A.aps_linear_workspace_bytes(BARE, M, N, K, T) == 0
+    Y = torch.empty(M, N, dtype=T, device=dev)
+    assert _raw(X, W, Y) == A.APS_OK
+    assert torch.equal(Y, A.aps_linear(X, W))
+    torch.cuda.synchronize()
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.memory_allocated()
+    A.aps_linear(X, W, Y=Y)
+    assert torch.cuda.max_memory_allocated() == before
+    # a workspace that is given is held to the size for any call
+    assert _raw(X, W, Y, torch.empty(64, dtype=torch.uint8, device=dev), 64) == A.APS_ERR_SIZE
+    X, W = _random(dev, T, (1, 65536), (16, 65536))
+    need = A.aps_linear_workspace_bytes(BARE, 1, 16, 65536, T)
+    assert need == A.aps_linear_workspace_bytes(A.APS_LINEAR_FORWARD, 1, 16, 65536, T) > 0
+    Y = torch.empty(1, 16, dtype=T, device=dev)
+    codes, exps = torch.empty(1, 16, dtype=torch.uint8, device=dev), torch.empty(1, 1, dtype=torch.int32, device=dev)
+    assert _raw(X, W, Y) == A.APS_ERR_NULL and _raw(X, W, Y, codes=codes, exps=exps) == A.APS_ERR_NULL
+    assert _raw(X, W, Y, torch.empty(need, dtype=torch.uint8, device=dev), need) == A.APS_OK
+    assert torch.equal(Y, A.aps_linear(X, W))
+    # off their chunks: whatever the kernel, the binding has what it takes
+    for n, k in ((4096, 1024), (16, 65536), (64, 200)):
+        x, w = _random(dev, T, (k + 1,), (n * k + 1,))
+        z, e = _bounds(x[1:].view(1, k), w[1:].view(n, k))
+        Y = A.aps_linear(x[1:].view(1, k), w[1:].view(n, k))
+        assert bool(((Y.double() - z).abs() <= e + R.half_step(T) * (z.abs() + e) + R.tiny(T)).all())
