@@ -275,7 +275,7 @@ __global__ __launch_bounds__(JTHREADS) void k_lin_join(LinArgs a) {
 LinTile lin_general(int op, int64_t np, int64_t nq, int64_t nc, bool f32) {
     static const struct {
         double stage, share;
-    } plain[] = {{2.0, 0.0022}, {1.7, 0.0036}}, decodes[] = {{3.6, 0.0125}, {2.3, 0.0072}};
+    } plain[] = {{2.0, 0.0022}, {1.4, 0.0036}}, decodes[] = {{3.6, 0.0125}, {2.3, 0.0072}};
     const auto& m = (op == OP_DW ? decodes : plain)[f32];
     const int64_t tiles = ((np + GP - 1) / GP) * ((nq + GQ - 1) / GQ);
     const int64_t split = std::max<int64_t>(1, std::min<int64_t>(512 / std::max<int64_t>(tiles, 1), nc / 128));
