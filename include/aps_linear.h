@@ -20,7 +20,7 @@
  * stride in elements, at least the row's length; pointers are aligned to
  * their element.  Rows of whole 16-byte chunks (8 or 4 elements, 16 codes)
  * that start on them (pointer and stride) run fastest; no alignment or length
- * is refused.
+ * is refused, others are copied or read in place.
  * Sizes: M, N, K in [0, 2^22] with every matrix at most 2^22 blocks of
  * 32 x 128 (2^34 elements); row strides up to 2^31 - 1.  Arrays that a
  * call does not touch (a dimension is 0) may be NULL.
@@ -68,7 +68,7 @@ extern "C" {
 enum { APS_DTYPE_F32 = 0, APS_DTYPE_BF16 = 1, APS_DTYPE_F16 = 2 };
 enum { APS_ACT_NONE = 0, APS_ACT_RELU = 1, APS_ACT_GELU = 2, APS_ACT_SILU = 3 };
 enum { APS_LINEAR_FORWARD = 0, APS_LINEAR_GRAD_INPUT = 1, APS_LINEAR_GRAD_WEIGHT = 2 };
-enum { APS_LINEAR_ON_CHUNKS = 4, APS_LINEAR_NO_CKPT = 8 }; /* aps_linear_workspace_bytes: added to op */
+enum { APS_LINEAR_ON_CHUNKS = 4, APS_LINEAR_NO_CKPT = 8, APS_LINEAR_OFF_CHUNKS = 16 }; /* aps_linear_workspace_bytes: added to op */
 #define APS_CKPT_ROWS 32
 #define APS_CKPT_COLS 128
 #define APS_CKPT_MAX_EXP 96
@@ -86,6 +86,11 @@ enum { APS_LINEAR_ON_CHUNKS = 4, APS_LINEAR_NO_CKPT = 8 }; /* aps_linear_workspa
  *                         are no whole ones: 0 where their call uses none; it
  *                         can then be made with workspace NULL and 0 bytes
  *   APS_LINEAR_NO_CKPT    of aps_linear without codes
+ *   APS_LINEAR_OFF_CHUNKS  of operands whose rows are whole chunks but do not
+ *                         all start on them (or lie 2^21 elements apart): more, where
+ *                         it pays to copy such an operand first.  With the bytes
+ *                         alone that every call needs it is read in place, up to
+ *                         eight times slower, its sums in another order
  */
 uint64_t aps_linear_workspace_bytes(int32_t op, int32_t M, int32_t N, int32_t K, int32_t dtype);
 

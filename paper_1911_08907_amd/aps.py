@@ -60,6 +60,7 @@ APS_LINEAR_GRAD_INPUT = 1
 APS_LINEAR_GRAD_WEIGHT = 2
 APS_LINEAR_ON_CHUNKS = 4
 APS_LINEAR_NO_CKPT = 8
+APS_LINEAR_OFF_CHUNKS = 16
 APS_CKPT_ROWS = 32
 APS_CKPT_COLS = 128
 APS_CKPT_MAX_EXP = 96
@@ -565,8 +566,8 @@ def _ckpt_out(M: int, C: int, codes, ckpt_exp, like, stream) -> tuple:
 
 def aps_linear_workspace_bytes(op: int, M: int, N: int, K: int, dtype) -> int:
     """Bytes of workspace of aps_linear (APS_LINEAR_FORWARD), aps_linear_grad_input
-    or aps_linear_grad_weight, with APS_LINEAR_ON_CHUNKS or APS_LINEAR_NO_CKPT
-    added or not; ``dtype`` is a torch dtype."""
+    or aps_linear_grad_weight, with APS_LINEAR_ON_CHUNKS, APS_LINEAR_OFF_CHUNKS
+    or APS_LINEAR_NO_CKPT added or not; ``dtype`` is a torch dtype."""
     if dtype not in _dtype_codes():
         raise ValueError(f"dtype must be float32, bfloat16 or float16, got {dtype}")
     return int(lib().aps_linear_workspace_bytes(int(op), int(M), int(N), int(K), _dtype_codes()[dtype]))
@@ -601,8 +602,7 @@ def _linear_workspace(op: int, M: int, N: int, K: int, dtype: int, workspace, Q,
     """(tensor, bytes) of the workspace of a product of Q and P; allocated where
     it is missing and needed."""
     if workspace is None:
-        if not (_off_chunks(Q, ldq) or _off_chunks(P, ldp)):
-            op |= APS_LINEAR_ON_CHUNKS
+        op |= APS_LINEAR_OFF_CHUNKS if _off_chunks(Q, ldq) or _off_chunks(P, ldp) else APS_LINEAR_ON_CHUNKS
         need = _linear_need(op, M, N, K, dtype)
         if need == 0:
             return None, 0

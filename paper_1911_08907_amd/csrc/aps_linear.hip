@@ -70,11 +70,10 @@ class Planner {
         if (empty_) return any();
         const bool f32 = dtype_ == APS_DTYPE_F32, rows = d_.nc > 0;
         // operands that the tile kernel would have to read from copies
-        const bool copy_p = rows && !whole_p(), copy_q = rows && !whole_q();
-        const bool off = rows && ((whole_p() && !on_p) || (whole_q() && !on_q));
+        const bool copy_p = rows && !(on_p && whole_p()), copy_q = rows && !(on_q && whole_q());
         // a copy's threads fit a launch
         const int64_t most = (int64_t)1 << 32;
-        const bool tile = tile_fits_ && !off && !(copy_p && rows_p(op_, d_) * row_p(op_, d_) > most) &&
+        const bool tile = tile_fits_ && !(copy_p && rows_p(op_, d_) * row_p(op_, d_) > most) &&
                           !(copy_q && rows_q(op_, d_) * row_q(op_, d_) > most);
         const bool few = op_ == OP_FWD && !keeps && d_.nq <= LIN_FEW;
         double us = 1e300;
@@ -91,12 +90,12 @@ class Planner {
         if (few) {
             // few rows leave the others no faster than the weights come from memory
             us = std::max(us, 3.0 + (double)d_.np * d_.nc * lin_elem_bytes(dtype_) / 3.6e6);
-            if (lin_decode_us(d_.np, d_.nq, d_.nc, f32, !(copy_p || copy_q || off)) <= us) best = {DECODE, 0, 1, false, false};
+            if (lin_decode_us(d_.np, d_.nq, d_.nc, f32, !(copy_p || copy_q)) <= us) best = {DECODE, 0, 1, false, false};
         }
         return best;
     }
 
-    // Bytes that suffice for every call.
+    // Bytes that suffice for every call, with no copy of an operand that is merely off its chunks.
     uint64_t need() const {
         return std::max(bytes_of(op_, d_, dtype_, plan(true, true, true)), bytes_of(op_, d_, dtype_, any()));
     }
@@ -157,13 +156,18 @@ int choose(int op, int dtype, const LinArgs& a, const void* w, uint64_t bytes, P
     const Dims d{a.np, a.nq, a.nc};
     const Planner planner(op, d, dtype);
     plan = planner.plan(a.codes != nullptr, on_chunks_p(op, dtype, a), on_chunks_q(dtype, a));
-    const uint64_t need = planner.need();
+    const uint64_t wants = bytes_of(op, d, dtype, plan), need = planner.need();
     const bool none = !w && bytes == 0;
-    if (need > 0 && !(none && bytes_of(op, d, dtype, plan) == 0)) {
+    if (need > 0 && !(none && wants == 0)) {
         if (!w) return APS_ERR_NULL;
         if (bytes < need) return APS_ERR_SIZE;
         if (!aligned16(w)) return APS_ERR_ALIGN;
     }
+    // operands off their chunks may be worth a copy that need() does not count
+    if (wants > (w ? bytes : 0))
+        plan = planner.any();
+    else if (wants > 0 && !aligned16(w))
+        return APS_ERR_ALIGN;
     return APS_OK;
 }
 
@@ -174,12 +178,16 @@ int choose(int op, int dtype, const LinArgs& a, const void* w, uint64_t bytes, P
 using namespace aps;
 
 extern "C" uint64_t aps_linear_workspace_bytes(int32_t op, int32_t M, int32_t N, int32_t K, int32_t dtype) {
-    const bool on = op & APS_LINEAR_ON_CHUNKS, keeps = !(op & APS_LINEAR_NO_CKPT);
-    op &= ~(APS_LINEAR_ON_CHUNKS | APS_LINEAR_NO_CKPT);
+    const bool on = op & APS_LINEAR_ON_CHUNKS, off = op & APS_LINEAR_OFF_CHUNKS, keeps = !(op & APS_LINEAR_NO_CKPT);
+    op &= ~(APS_LINEAR_ON_CHUNKS | APS_LINEAR_OFF_CHUNKS | APS_LINEAR_NO_CKPT);
     if (op < OP_FWD || op > OP_DW || lin_check_dims(M, N, K, dtype) != APS_OK) return 0;
     const Dims d = dims_of(op, M, N, K);
     const Planner planner(op, d, dtype);
-    return on && bytes_of(op, d, dtype, planner.plan(keeps, true, true)) == 0 ? 0 : planner.need();
+    if (on && bytes_of(op, d, dtype, planner.plan(keeps, true, true)) == 0) return 0;
+    uint64_t bytes = planner.need();
+    for (int ons = 0; off && ons < 3; ++ons)  // P, Q or both off their chunks
+        bytes = std::max(bytes, bytes_of(op, d, dtype, planner.plan(keeps, ons & 1, ons & 2)));
+    return bytes;
 }
 
 extern "C" int aps_linear(const void* X, int64_t ldx, const void* W, int64_t ldw, const void* bias, const void* R,

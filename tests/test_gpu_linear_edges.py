@@ -183,3 +183,65 @@ def test_few_rows_need_no_workspace(dev, t):
         z, e = _bounds(x[1:].view(1, k), w[1:].view(n, k))
         Y = A.aps_linear(x[1:].view(1, k), w[1:].view(n, k))
         assert bool(((Y.double() - z).abs() <= e + R.half_step(T) * (z.abs() + e) + R.tiny(T)).all())
+
+
+# ------------------------------------------------- operands off their chunks
+
+def _shifted(x, layout):
+    """The matrix x at an address or with a stride that is no whole chunk."""
+    M, C = x.shape
+    if layout == "address":
+        b = torch.full((M * C + 1,), -1 if x.dtype == torch.uint8 else math.nan, device=x.device).to(x.dtype)
+        v = b[1:].view(M, C)
+    else:
+        b = torch.full((M, C + 5), 255 if x.dtype == torch.uint8 else math.nan, device=x.device).to(x.dtype)
+        v = b[:, :C]
+    v.copy_(x)
+    return v
+
+
+@pytest.mark.parametrize("layout", ["address", "stride"])
+@pytest.mark.parametrize("t", list(TYPES))
+def test_large_products_off_their_chunks(dev, t, layout):
+    """Products large enough for a copy to pay have the sums of aligned operands,
+    to the last bit, whichever operand is off; with the bytes alone that every call
+    needs they are read in place, within the sums' bound."""
+    T = TYPES[t]
+    M, N, K = 1024, 1280, 1536
+    X, W, b, r, dZ = _random(dev, T, (M, K), (N, K), (N,), (M, N), (M, N))
+    cx, wx = A.aps_checkpoint_save(X, FMT["1-4-3"])
+    Y, cz, wz = A.aps_linear(X, W, b, r, ACT["silu"], ckpt_fmt=FMT["1-5-2"])
+    dX = A.aps_linear_grad_input(dZ, W, X, ACT["gelu"], cx, wx, FMT["1-4-3"])
+    db, db1 = torch.empty(N, device=dev), torch.empty(N, device=dev)
+    dW = A.aps_linear_grad_weight(dZ, cx, wx, FMT["1-4-3"], dbias=db)
+    Xs, Ws, dZs, cxs = (_shifted(v, layout) for v in (X, W, dZ, cx))
+    for x, w in ((Xs, W), (X, Ws), (Xs, Ws)):
+        y, c, e = A.aps_linear(x, w, b, r, ACT["silu"], ckpt_fmt=FMT["1-5-2"])
+        assert torch.equal(y, Y) and torch.equal(c, cz) and torch.equal(e, wz)
+        assert torch.equal(A.aps_linear(x, w, b, r, ACT["silu"]), Y)
+    for d, w in ((dZs, W), (dZ, Ws), (dZs, Ws)):
+        assert torch.equal(A.aps_linear_grad_input(d, w, X, ACT["gelu"], cx, wx, FMT["1-4-3"]), dX)
+    for d, c in ((dZs, cx), (dZ, cxs), (dZs, cxs)):
+        assert torch.equal(A.aps_linear_grad_weight(d, c, wx, FMT["1-4-3"], dbias=db1), dW) and torch.equal(db, db1)
+
+
+@pytest.mark.parametrize("t", list(TYPES))
+def test_workspaces_of_operands_off_their_chunks(dev, t):
+    """With the bytes that the flag asks for, the operands are copied; with those
+    alone that every call needs (here none) they are read in place, within the
+    sums' bound; nothing behind the workspace is written."""
+    T = TYPES[t]
+    M, N, K = 4096, 2048, 512
+    X, W = _random(dev, T, (M, K), (N, K))
+    Xs, Ws = _shifted(X, "address"), _shifted(W, "stride")
+    need = A.aps_linear_workspace_bytes(A.APS_LINEAR_FORWARD, M, N, K, T)
+    off = A.aps_linear_workspace_bytes(A.APS_LINEAR_FORWARD | A.APS_LINEAR_OFF_CHUNKS, M, N, K, T)
+    assert off > need == 0
+    Y = torch.empty(M, N, dtype=T, device=dev)
+    assert _raw(Xs, Ws, Y) == A.APS_OK
+    z, e = _bounds(X, W)
+    assert bool(((Y.double() - z).abs() <= e + R.half_step(T) * (z.abs() + e) + R.tiny(T)).all())
+    marked = torch.full((off + 256,), 0xA5, dtype=torch.uint8, device=dev)
+    assert torch.equal(A.aps_linear(Xs, Ws, workspace=marked[:off]), A.aps_linear(X, W))
+    assert bool((marked[off:] == 0xA5).all())
+    assert _raw(Xs, Ws, Y, marked[8:], off) == A.APS_ERR_ALIGN

@@ -34,7 +34,18 @@ def test_calls_without_a_checkpoint(lib, dt):
         assert w(op | ON, *((64, 64, 65536), (64, 65536, 64), (65536, 64, 64))[op], dt) > 0
         assert w(op | A.APS_LINEAR_NO_CKPT, 8, 4096, 1024, dt) == w(op, 8, 4096, 1024, dt)
     # no operations
-    assert w(3 | ON, 8, 64, 65536, dt) == 0 and w(32, 8, 64, 65536, dt) == 0 and w(-1, 8, 64, 65536, dt) == 0
+    assert w(3 | ON, 8, 64, 65536, dt) == 0 and w(64, 8, 64, 65536, dt) == 0 and w(-1, 8, 64, 65536, dt) == 0
+
+
+@pytest.mark.parametrize("op", range(3))
+def test_operands_off_their_chunks(lib, op):
+    """More bytes where a copy pays: at most both operands' and the sums'."""
+    w, off = lib.aps_linear_workspace_bytes, A.APS_LINEAR_OFF_CHUNKS
+    assert w(op | off, 4096, 4096, 4096, BF16) >= w(op, 4096, 4096, 4096, BF16) + 4096 * 4096
+    for M, N, K in ((1, 1, 1), (1, 4096, 1024), (40, 256, 128), (333, 1000, 520), (2000, 1001, 64), (0, 8, 8), (8, 8, 0)):
+        for dt in (BF16, F16, F32):
+            base, more = w(op, M, N, K, dt), w(op | off, M, N, K, dt)
+            assert base <= more <= base + (M * N + N * K + M * K) * 4 + 64 * max(1, M, N, K) + 1024 + base
 
 
 @no_gpu
