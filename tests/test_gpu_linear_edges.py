@@ -245,3 +245,155 @@ def test_workspaces_of_operands_off_their_chunks(dev, t):
     assert torch.equal(A.aps_linear(Xs, Ws, workspace=marked[:off]), A.aps_linear(X, W))
     assert bool((marked[off:] == 0xA5).all())
     assert _raw(Xs, Ws, Y, marked[8:], off) == A.APS_ERR_ALIGN
+
+
+# ------------------------------------------------- exact results
+
+# few rows whole and in pieces, tiles of every size whole and in pieces, rows
+# that are copied or read one element at a time, partial tiles on every side
+EXACT = [(1, 1, 1), (3, 40, 72), (5, 16, 8192), (40, 256, 128), (64, 1024, 4096), (77, 130, 1001), (300, 130, 101),
+         (520, 333, 2050), (700, 1000, 520), (2100, 1032, 136)]
+
+
+@pytest.mark.parametrize("M,N,K", EXACT)
+@pytest.mark.parametrize("t", list(TYPES))
+def test_sums_that_fp32_holds_come_out_exact(dev, t, M, N, K):
+    """Quarters and eighths of small whole numbers: every partial sum is a
+    multiple of 2^-5 below 2^12, so any order of them is exact, and the stored
+    results and the checkpoint's codes are those of the float64 values."""
+    T = TYPES[t]
+    g = torch.Generator().manual_seed(M + N + K)
+    draw = lambda *s: torch.randint(-4, 5, s, generator=g).double()  # noqa: E731
+    X, W, b, r, dZ = draw(M, K) / 4, draw(N, K) / 8, draw(N) / 2, draw(M, N), draw(M, N) / 4
+    put = lambda v: v.to(T).to(dev)  # noqa: E731
+    log("exact", t, M, N, K)
+    z = (X @ W.t() if K < 5000 else (X.to(dev) @ W.to(dev).t()).cpu()) + b
+    fmt = "1-4-3" if K % 2 else "1-5-2"
+    Y, codes, words = A.aps_linear(put(X), put(W), put(b), put(r), ACT["relu"], ckpt_fmt=FMT[fmt])
+    want = (z.clamp(min=0) + r).float().to(T)
+    assert torch.equal(Y.cpu(), want) and torch.equal(A.aps_linear(put(X), put(W), put(b), put(r), ACT["relu"]).cpu(), want)
+    rc, rw = R.save(z, fmt, T)
+    zero = z == 0  # a sum of both signs' zeros may be either
+    assert torch.equal(codes.cpu()[~zero], rc[~zero]) and not bool((codes.cpu()[zero] & 127).any())
+    assert torch.equal(words.cpu(), rw)
+    cx, wx = A.aps_checkpoint_save(put(X), FMT[fmt])
+    assert torch.equal(A.aps_checkpoint_load(cx, wx, FMT[fmt], dtype=T).cpu(), X.to(T))
+    bypass = draw(M, K)
+    want = ((dZ @ W) * (X > 0) + bypass).float().to(T)
+    assert torch.equal(A.aps_linear_grad_input(put(dZ), put(W), put(bypass), ACT["relu"], cx, wx, FMT[fmt]).cpu(), want)
+    dX = put(bypass)  # in place of the residual
+    A.aps_linear_grad_input(put(dZ), put(W), dX, ACT["relu"], cx, wx, FMT[fmt], dX)
+    assert torch.equal(dX.cpu(), want)
+    db = torch.empty(N, device=dev)
+    dW = A.aps_linear_grad_weight(put(dZ), cx, wx, FMT[fmt], dbias=db)
+    assert torch.equal(dW.cpu().double(), dZ.t() @ X) and torch.equal(db.cpu().double(), dZ.sum(0))
+    A.aps_linear_grad_weight(put(dZ), cx, wx, FMT[fmt], dW, db, accumulate=True)
+    assert torch.equal(dW.cpu().double(), 2 * (dZ.t() @ X)) and torch.equal(db.cpu().double(), 2 * dZ.sum(0))
+
+
+@pytest.mark.parametrize("layout", ["dense", "padded", "odd"])
+@pytest.mark.parametrize("t", list(TYPES))
+def test_input_gradient_in_place_of_its_residual(dev, t, layout):
+    """dX = R, whole and in pieces, in every layout of its rows."""
+    T = TYPES[t]
+    for M, N, K in ((1, 64, 40), (64, 4096, 512), (300, 101, 130), (512, 256, 520)):
+        log("in place", t, layout, M, N, K)
+        dZ, W, r, x = _random(dev, T, (M, N), (N, K), (M, K), (M, K))
+        c, w = A.aps_checkpoint_save(x, FMT["1-4-3"])
+        ld, at = {"dense": (K, 0), "padded": (-(-(K + 1) // 8) * 8, 8), "odd": (K + 3, 1)}[layout]
+        buf = torch.full((M * ld + at + ld,), 77.0, dtype=T, device=dev)
+        v = buf[at:at + M * ld].view(M, ld)[:, :K]
+        v.copy_(r)
+        want = A.aps_linear_grad_input(dZ, W, r, ACT["gelu"], c, w, FMT["1-4-3"])
+        assert A.aps_linear_grad_input(dZ, W, v, ACT["gelu"], c, w, FMT["1-4-3"], v) is v
+        assert torch.equal(v, want)
+        v.fill_(77.0)
+        assert bool((buf == 77.0).all())
+
+
+# ------------------------------------------------- the ends of the types
+
+@pytest.mark.parametrize("t", ["bf16", "fp16"])
+def test_subnormal_gradients_and_checkpoints_count(dev, t):
+    """Column sums and weight gradients of subnormal dZ, and of checkpoints that
+    stand for subnormal halves: nothing is flushed."""
+    T = TYPES[t]
+    small = torch.finfo(T).smallest_normal / 4
+    for M, N, K in ((64, 128, 128), (64, 127, 101), (33, 64, 64), (300, 520, 264)):
+        log("subnormal", t, M, N, K)
+        for fmt in FMT:
+            dZ, x = torch.full((M, N), small, dtype=T, device=dev), torch.ones(M, K, dtype=T, device=dev)
+            db = torch.empty(N, device=dev)
+            dW = A.aps_linear_grad_weight(dZ, *A.aps_checkpoint_save(x, FMT[fmt]), FMT[fmt], dbias=db)
+            assert bool((dW.double() == M * small).all()) and bool((db.double() == M * small).all())
+            x = torch.full((M, K), 2.0 ** -20, dtype=T, device=dev)
+            c, w = A.aps_checkpoint_save(x, FMT[fmt])
+            assert torch.equal(A.aps_checkpoint_load(c, w, FMT[fmt], dtype=T), x)
+            dW = A.aps_linear_grad_weight(torch.ones_like(dZ), c, w, FMT[fmt])
+            assert bool((dW.double() == M * 2.0 ** -20).all())
+
+
+@pytest.mark.parametrize("act", list(ACT))
+@pytest.mark.parametrize("fmt", list(FMT))
+@pytest.mark.parametrize("t", list(TYPES))
+def test_infinite_results(dev, t, fmt, act):
+    """Where an activation is +-INF, or past the type's range, the result is INF of
+    its sign; everywhere else it is finite: from codes, and from z itself."""
+    T = TYPES[t]
+    codes = torch.arange(256, dtype=torch.uint8).repeat(64, 1)
+    words = torch.tensor([[3, (-4 & 0xFFFF)], [0, 12]], dtype=torch.int32) | (1 << 16)
+    ref = R.act(R.load(codes, words, fmt), act)
+    # rounds to INF from half a step above the largest value on
+    end = torch.finfo(T).max * (1 + torch.finfo(T).eps / 4)
+    inf, nan = ref.abs() >= end, torch.isnan(ref)
+    Z = A.aps_checkpoint_load(codes.to(dev), words.to(dev), FMT[fmt], ACT[act], dtype=T).cpu()
+    assert bool(inf.any()) and torch.equal(Z[inf].double(), torch.sign(ref[inf]) * math.inf)
+    assert bool(torch.isfinite(Z[~inf & ~nan]).all()) and bool(torch.isnan(Z[nan]).all())
+    z = torch.tensor([math.inf, -math.inf, math.nan, 1.0, -1.0, 0.0, torch.finfo(T).max, -torch.finfo(T).max], dtype=T)
+    ref = R.act(z.double(), act)
+    for M in (1, 40):
+        Y = A.aps_linear(torch.zeros(M, 0, dtype=T, device=dev), torch.zeros(8, 0, dtype=T, device=dev), z.to(dev), None,
+                         ACT[act]).cpu().double()
+        assert torch.equal(torch.isnan(Y), torch.isnan(ref).expand(M, 8))
+        assert torch.equal(torch.where(torch.isinf(Y), Y, 0.0).nan_to_num(0.0), torch.where(torch.isinf(ref), ref, 0.0).nan_to_num(0.0).expand(M, 8))
+    s = R.slope(torch.tensor([math.inf, -math.inf], dtype=torch.float64), act).to(T)
+    c, w = A.aps_checkpoint_save(torch.tensor([[math.inf, -math.inf]], dtype=T, device=dev), FMT[fmt])
+    one = torch.ones(1, 2, dtype=T, device=dev)
+    assert torch.equal(A.aps_activation_grad(one, c, w, FMT[fmt], ACT[act]).cpu()[0], s)
+
+
+# ------------------------------------------------- the same call again
+
+def test_results_do_not_depend_on_the_launch(dev):
+    """The same large products, alone and with others in flight: the same bits.
+    Against float64 the checkpoint's codes differ only where z lies within its
+    sum's error of a border between two codes."""
+    M, N, K = 4096, 4096, 1024
+    X, W, b, dZ = _random(dev, torch.bfloat16, (M, K), (N, K), (N,), (M, N))
+    F = FMT["1-4-3"]
+    run = lambda: A.aps_linear(X, W, b, None, ACT["gelu"], ckpt_fmt=F)  # noqa: E731
+    Y, codes, words = run()
+    back = lambda: A.aps_linear_grad_weight(dZ, *cx, F)  # noqa: E731
+    cx = A.aps_checkpoint_save(X, F)
+    dW = back()
+    other = torch.cuda.Stream()
+    other.wait_stream(torch.cuda.current_stream())
+    for k in range(12):
+        if k % 2:
+            with torch.cuda.stream(other):
+                torch.mm(X, W.t())
+        y, c, w = run()
+        assert torch.equal(y, Y) and torch.equal(c, codes) and torch.equal(w, words) and torch.equal(back(), dW)
+    torch.cuda.synchronize()
+    z, e = _bounds(X, W, b)
+    ft = ((words.long() & 0xFFFF) ^ 0x8000) - 0x8000
+    s = z * torch.exp2(R.spread(ft.cpu().double(), M, N, dev))
+    e = e * torch.exp2(R.spread(ft.cpu().double(), M, N, dev))
+    got = R.table("1-4-3").to(dev)[codes.long()]
+    step = torch.exp2(torch.floor(torch.log2(s.abs().clamp(min=2.0 ** -6))) - 3)
+    near = torch.round(s / step) * step
+    other_code = got != near
+    # the nearest border of z's own interval lies within the bound
+    border = (s / step - torch.floor(s / step) - 0.5).abs() * step
+    assert bool((border[other_code] <= e[other_code]).all())
+    assert int(other_code.sum()) < 1000
