@@ -192,8 +192,9 @@ __global__ __launch_bounds__(CTHREADS) void k_ckpt_save(CkArgs a) {
 }
 
 // GRAD: out = X * act'(z); otherwise out = act(z), z the checkpoint's values.
-// 16384 x 4096 bf16 loads in 30 us, and GELU's gradient of 8192 x 4096 takes 30
-// (5.6 TB/s): bound by HBM; a few rows by latency, 4 us.
+// 16384 x 4096 bf16 loads in 30 us, and GELU's gradient of 8192 x 4096 takes 31
+// (5.4 TB/s): bound by HBM; a few rows by latency, 4 us.  In fp32 GELU's 33
+// operations bound it: 8192 x 4096 loads in 41 us, its gradient takes 52.
 // A wave takes LOAD_STEPS of a block's steps: nothing ties the rows together,
 // and more waves hide the activations' arithmetic and a few rows' latency.
 template <class T, bool E5, bool VEC, bool GRAD>
