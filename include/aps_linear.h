@@ -82,15 +82,16 @@ enum { APS_LINEAR_ON_CHUNKS = 4, APS_LINEAR_NO_CKPT = 8, APS_LINEAR_OFF_CHUNKS =
  * chunks.  They suffice for every such call, and a workspace that is given
  * holds at least as many.  0 where none needs any, and for arguments out of
  * range.  Host-only.  Flags can be added to op:
- *   APS_LINEAR_ON_CHUNKS  of operands whose rows start on 16-byte chunks, or
- *                         are no whole ones: 0 where their call uses none; it
- *                         can then be made with workspace NULL and 0 bytes
- *   APS_LINEAR_NO_CKPT    of aps_linear without codes
- *   APS_LINEAR_OFF_CHUNKS  of operands whose rows are whole chunks but do not
- *                         all start on them (or lie 2^21 elements apart): more, where
- *                         it pays to copy such an operand first.  With the bytes
- *                         alone that every call needs it is read in place, up to
- *                         eight times slower, its sums in another order
+ *   APS_LINEAR_ON_CHUNKS   of operands whose rows start on 16-byte chunks, less
+ *                          than 2^21 elements apart, or are no whole ones: 0
+ *                          where their call uses none; it can then be made
+ *                          with workspace NULL and 0 bytes
+ *   APS_LINEAR_OFF_CHUNKS  of operands whose rows are whole chunks but do not all
+ *                          start on them, or lie further apart: more, where it
+ *                          pays to copy such an operand first.  With the bytes
+ *                          alone that every call needs it is read in place, up
+ *                          to eight times slower, its sums in another order
+ *   APS_LINEAR_NO_CKPT     of aps_linear without codes
  */
 uint64_t aps_linear_workspace_bytes(int32_t op, int32_t M, int32_t N, int32_t K, int32_t dtype);
 

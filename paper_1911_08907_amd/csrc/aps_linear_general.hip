@@ -268,8 +268,8 @@ __global__ __launch_bounds__(JTHREADS) void k_lin_join(LinArgs a) {
 // per CU, enough pieces for that many, of at least 128 contraction elements:
 // up to 512.  The time in us: a launch; per stage of 64 bytes its latency or its
 // share for each tile at work; for a split the join's launch, its serial sum and
-// the partial sums' way out and in.  Fitted to graph replays of 240 products (a
-// third of them with rows off their chunks): two stages take 8.7, 1444 x 1472 of
+// the partial sums' way out and in.  Fitted to graph replays of 240 products,
+// half of them with rows off their chunks: two stages take 8.7, 1444 x 1472 of
 // 64 10.1, 8000 x 4095 of 4095 894, bf16; a weight gradient of 4868 rows,
 // 256 x 3264, 234; 21568 in 168 pieces, fp32, 32.
 LinTile lin_general(int op, int64_t np, int64_t nq, int64_t nc, bool f32) {
