@@ -591,23 +591,21 @@ def _linear_need(op: int, M: int, N: int, K: int, dtype: int) -> int:
     return int(lib().aps_linear_workspace_bytes(op, M, N, K, dtype))
 
 
-def _off_chunks(t, ld: int) -> bool:
+def _off_chunks(pointer: int, ld: int, cols: int, each: int) -> bool:
     """Whether rows of whole 16-byte chunks do not all start on them, or further
     apart than the library's tiles take."""
-    each = t.element_size()
-    return t.shape[1] * each & 15 == 0 and ((t.data_ptr() | ld * each) & 15 != 0 or ld >= 1 << 21)
+    return not cols * each & 15 and ((pointer | ld * each) & 15 != 0 or ld >= 1 << 21)
 
 
-def _linear_workspace(op: int, M: int, N: int, K: int, dtype: int, workspace, Q, ldq: int, P, ldp: int, stream):
-    """(tensor, bytes) of the workspace of a product of Q and P; allocated where
-    it is missing and needed."""
+def _linear_workspace(op: int, M: int, N: int, K: int, dtype: int, off: bool, workspace, like, stream):
+    """(tensor, bytes) of the call's workspace; allocated where it is missing and
+    needed.  ``off``: of an operand off its chunks."""
     if workspace is None:
-        op |= APS_LINEAR_OFF_CHUNKS if _off_chunks(Q, ldq) or _off_chunks(P, ldp) else APS_LINEAR_ON_CHUNKS
-        need = _linear_need(op, M, N, K, dtype)
+        need = _linear_need(op | (APS_LINEAR_OFF_CHUNKS if off else APS_LINEAR_ON_CHUNKS), M, N, K, dtype)
         if need == 0:
             return None, 0
-        return _fresh(Q, need, stream, _dtypes(*_U8)[0]), need
-    _need(workspace, "workspace", _dtypes(*_U8), 0, Q.device)
+        return _fresh(like, need, stream, _dtypes(*_U8)[0]), need
+    _need(workspace, "workspace", _dtypes(*_U8), 0, like.device)
     return workspace, workspace.numel()
 
 
@@ -644,9 +642,11 @@ def aps_linear(X, W, bias=None, residual=None, act: int = APS_ACT_NONE, Y=None, 
     elif codes is not None or ckpt_exp is not None:
         raise ValueError("codes and ckpt_exp need ckpt_fmt")
     op = APS_LINEAR_FORWARD if ckpt_fmt is not None else APS_LINEAR_FORWARD | APS_LINEAR_NO_CKPT
-    ws, nbytes = _linear_workspace(op, M, N, K, dt, workspace, X, ldx, W, ldw, stream)
+    px, pw, each = X.data_ptr(), W.data_ptr(), 4 if dt == APS_DTYPE_F32 else 2
+    off = _off_chunks(px, ldx, K, each) or _off_chunks(pw, ldw, K, each)
+    ws, nbytes = _linear_workspace(op, M, N, K, dt, off, workspace, X, stream)
     _check("aps_linear", lib().aps_linear(
-        _ptr(X), ldx, _ptr(W), ldw, _ptr(bias), _ptr(residual), ldr, _ptr(Y), ldy, M, N, K, dt, int(act),
+        px, ldx, pw, ldw, _ptr(bias), _ptr(residual), ldr, _ptr(Y), ldy, M, N, K, dt, int(act),
         _NO_FORMAT if ckpt_fmt is None else ckpt_fmt.c(), _ptr(codes), ldc, _ptr(ckpt_exp), _ptr(ws), nbytes,
         _stream(stream, dev)))
     return Y if ckpt_fmt is None else (Y, codes, ckpt_exp)
@@ -675,9 +675,11 @@ def aps_linear_grad_input(dZ, W, residual=None, act: int = APS_ACT_NONE, codes=N
         ldc = _ckpt(codes, ckpt_exp, dev, (M, K))
     elif codes is not None or ckpt_exp is not None or fmt is not None:
         raise ValueError("a checkpoint is read for an activation's derivative only: act is none")
-    ws, nbytes = _linear_workspace(APS_LINEAR_GRAD_INPUT, M, N, K, dt, workspace, dZ, ldz, W, ldw, stream)
+    pz, pw, each = dZ.data_ptr(), W.data_ptr(), 4 if dt == APS_DTYPE_F32 else 2
+    off = _off_chunks(pz, ldz, N, each) or _off_chunks(pw, ldw, K, each)
+    ws, nbytes = _linear_workspace(APS_LINEAR_GRAD_INPUT, M, N, K, dt, off, workspace, dZ, stream)
     _check("aps_linear_grad_input", lib().aps_linear_grad_input(
-        _ptr(dZ), ldz, _ptr(W), ldw, _ptr(residual), ldr, int(act), _NO_FORMAT if fmt is None else fmt.c(),
+        pz, ldz, pw, ldw, _ptr(residual), ldr, int(act), _NO_FORMAT if fmt is None else fmt.c(),
         _ptr(codes), ldc, _ptr(ckpt_exp), _ptr(dX), ldx, M, N, K, dt, _ptr(ws), nbytes, _stream(stream, dev)))
     return dX
 
@@ -701,9 +703,11 @@ def aps_linear_grad_weight(dZ, codes, ckpt_exp, fmt: Format, dW=None, dbias=None
     else:
         lddw = _matrix(dW, "dW", _dtypes(*_F32), dev, (N, K))
     _need(dbias, "dbias", _dtypes(*_F32), N, dev, optional=True)
-    ws, nbytes = _linear_workspace(APS_LINEAR_GRAD_WEIGHT, M, N, K, dt, workspace, dZ, ldz, codes, ldc, stream)
+    pz, pc = dZ.data_ptr(), codes.data_ptr()
+    off = _off_chunks(pz, ldz, N, 4 if dt == APS_DTYPE_F32 else 2) or _off_chunks(pc, ldc, K, 1)
+    ws, nbytes = _linear_workspace(APS_LINEAR_GRAD_WEIGHT, M, N, K, dt, off, workspace, dZ, stream)
     _check("aps_linear_grad_weight", lib().aps_linear_grad_weight(
-        _ptr(dZ), ldz, fmt.c(), _ptr(codes), ldc, _ptr(ckpt_exp), _ptr(dW), lddw, _ptr(dbias), M, N, K, dt,
+        pz, ldz, fmt.c(), pc, ldc, _ptr(ckpt_exp), _ptr(dW), lddw, _ptr(dbias), M, N, K, dt,
         APS_GRAD_ACCUMULATE if accumulate else 0, _ptr(ws), nbytes, _stream(stream, dev)))
     return dW
 

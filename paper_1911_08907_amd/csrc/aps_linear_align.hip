@@ -37,11 +37,10 @@ __global__ __launch_bounds__(256) void k_lin_align(LinCopy p, LinCopy q, int64_t
 
 }  // namespace
 
-// A launch more, the host's share of it too (77 x 777 x 1001 fp32 in three launches
-// took 30 us a call, in two 27, and in a graph 21 either way), then the copies
-// at 1.5 TB/s of what they write: in a trace 0.3 MB take 3.6 us, 2.2 MB 4.4, and of
-// bf16 off its chunks 34 MB 25 us, 168 MB 114; fp32 up to 2.4 TB/s (336 MB 140 us).
-double lin_align_us(uint64_t bytes) { return 8.0 + (double)bytes / 1.5e6; }
+// The launch and what it adds to a sequence of kernels, then the copies at 1.5 TB/s
+// of what they write: in a trace 0.3 MB take 3.6 us, 2.2 MB 4.4, and of bf16 off
+// its chunks 34 MB 25 us, 168 MB 114; fp32 copies up to 2.4 TB/s (336 MB 140 us).
+double lin_align_us(uint64_t bytes) { return 6.0 + (double)bytes / 1.5e6; }
 
 void launch_lin_align(const LinCopy& p, const LinCopy& q, hipStream_t s) {
     const auto chunks = [](const LinCopy& c) { return c.src ? c.rows * (c.ldd * c.elem / 16) : 0; };

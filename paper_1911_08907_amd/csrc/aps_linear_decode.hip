@@ -102,8 +102,7 @@ __global__ __launch_bounds__(64 * DWAVES) void k_lin_decode(LinArgs a) {
 // another, whose latency grows with the rows of q, the workgroups' shares of the
 // memory's rate, and a workgroup's start.  Element by element (off chunks) all of
 // it costs more.  Fitted to graph replays of 220 products beside the other
-// kernels; in 220 others the choice missed the fastest by 3 % on average.  In us, this
-// kernel and the best of the others:
+// kernels.  In us, this kernel and the best of the others:
 //                            1 row         8             32
 //   4096 x 1024 bf16         4.8, 8.3      4.8, 8.2      6.1, 8.9
 //   ... off chunks           12.3, 9.7     16.0, 9.9     25.1, 11.3

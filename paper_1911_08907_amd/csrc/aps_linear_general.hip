@@ -266,22 +266,23 @@ __global__ __launch_bounds__(JTHREADS) void k_lin_join(LinArgs a) {
 
 // Pieces of the contraction: where the tiles are fewer than two workgroups
 // per CU, enough pieces for that many, of at least 128 contraction elements:
-// up to 512.  The time in us: a launch; per stage of 64 bytes its latency or its
-// share for each tile at work; for a split the join's launch, its serial sum and
-// the partial sums' way out and in.  Fitted to graph replays of 240 products,
-// half of them with rows off their chunks: two stages take 8.7, 1444 x 1472 of
-// 64 10.1, 8000 x 4095 of 4095 894, bf16; a weight gradient of 4868 rows,
-// 256 x 3264, 234; 21568 in 168 pieces, fp32, 32.
+// up to 512.  The time in us: a launch and the first stage's way in; per stage of
+// 64 bytes its latency or its share for each tile at work; for a split the join's
+// launch, its serial sum and the partial sums' way out and in.  Fitted to graph
+// replays of 480 products, half of them with rows off their chunks, beside the
+// other kernels: two stages take 8.7, 118 x 2307 of 7669 in 13 pieces 41, 8000 x
+// 4095 of 4095 894, bf16; a weight gradient of 4868 rows, 256 x 3264, 234; 21568
+// in 168 pieces, fp32, 32.
 LinTile lin_general(int op, int64_t np, int64_t nq, int64_t nc, bool f32) {
     static const struct {
         double stage, share;
-    } plain[] = {{2.0, 0.0022}, {1.4, 0.0036}}, decodes[] = {{3.6, 0.0125}, {2.3, 0.0072}};
+    } plain[] = {{1.3, 0.0025}, {1.1, 0.0036}}, decodes[] = {{3.3, 0.0115}, {2.1, 0.0073}};
     const auto& m = (op == OP_DW ? decodes : plain)[f32];
     const int64_t tiles = ((np + GP - 1) / GP) * ((nq + GQ - 1) / GQ);
     const int64_t split = std::max<int64_t>(1, std::min<int64_t>(512 / std::max<int64_t>(tiles, 1), nc / 128));
     const int64_t stages = (nc + (f32 ? 15 : 31)) / (f32 ? 16 : 32);
-    const double us = 4.5 + std::ceil((double)stages / split) * std::max(m.stage, m.share * tiles * split) +
-                      (split > 1 ? 4.0 + 0.08 * split + (double)split * np * nq * 8 / 6.0e6 : 0.0);
+    const double us = 6.5 + std::ceil((double)stages / split) * std::max(m.stage, m.share * tiles * split) +
+                      (split > 1 ? 2.0 + 0.08 * split + (double)split * np * nq * 8 / 6.0e6 : 0.0);
     return {LIN_SMALL, (int)split, us};
 }
 
